@@ -19,8 +19,10 @@
  * dhsa_sparse_prefill, dhsa_prefill runs both on one stream.
  * Beside the path: dhsa_finalize_boundaries (boundary scores -> B, Sec. 3.2),
  * dhsa_recall_rows (recall of the routed sets against exact top-k attention),
- * dhsa_decode_step (the newest token's row alone, over cached K / V), and the
- * inspection hooks dhsa_plan_expand_rows, dhsa_debug_routing, dhsa_mfma_probe.
+ * dhsa_decode_step (the newest token's row alone, over cached K / V), the
+ * inspection hooks dhsa_plan_expand_rows, dhsa_debug_routing, dhsa_mfma_probe,
+ * and attention without routing: dhsa_window_prefill (the last keys and the
+ * first ones) and the paged cache of dhsa_paged_append / _attend / _evict.
  *
  * With B_r > 0 in the problem struct the same entry points run Alg. 1 as it is
  * printed (App. C) instead of the per-row form above: queries are grouped in
@@ -349,8 +351,100 @@ dhsa_status dhsa_decode_step(const dhsa_problem *prob, const void *Q_dev, const 
 /* 0 if the problem's scalar fields or the caps are out of range. */
 size_t dhsa_decode_workspace_bytes(const dhsa_problem *prob, int32_t N_c_cap, int64_t L_cap);
 
+/* ---- attention without routing: a window of last keys, a paged cache ---- */
+
+/* Dense causal attention of a prompt in which a row keeps sight of its surroundings
+ * and of the beginning only: row i attends to the keys j <= i with i - j < window or
+ * j < sinks; O_dev[h, i, :] = softmax over them of q_i . k_j scale, times V.
+ * window >= 1 (window >= L: all keys j <= i), sinks >= 0 (else DHSA_ERR_SHAPE).  Of
+ * `prob` the fields L, H_q, H_kv, D, dtype, scale and the strides are used; N_c, N_b,
+ * B_r and pooling are not.  What the limits of dhsa_prefill say holds, and for
+ * DHSA_F32 one K or V head must span less than 64 GiB.  No workspace. */
+dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t window, int64_t sinks, const void *Q_dev,
+                                const void *K_dev, const void *V_dev, void *O_dev, void *stream);
+
+/* K and V rows of several sequences in pages of one pool, and the new tokens of a call.
+ *   K, V   [n_pages][H_kv][page_size][D], D contiguous, with the strides below
+ *   table  int32 [n_seq][max_pages], device: page of slots [p page_size, (p + 1) page_size)
+ *          of a sequence.  A contiguous cache [H_kv][L][D] is one page of L slots.
+ *   kv_len int32 [n_seq], device: tokens of each sequence, the new ones included; they are
+ *          in the slots 0 .. kv_len - 1, older ones first.
+ *   q_start int32 [n_seq + 1], device: the new tokens of sequence s are the rows
+ *          q_start[s] .. q_start[s + 1] - 1 of Q, O and of the new K and V, n_s of them
+ *          (0 or more), in the slots kv_len[s] - n_s .. kv_len[s] - 1.  Not descending, from 0.
+ * These arrays are read by the kernels when the call runs: a captured graph may be replayed
+ * with other lengths and pages in them, as long as n_seq and T bound what is there.  They
+ * are not validated on the host; what the kernels find is clamped: rows behind T and slots
+ * behind max_pages page_size are not touched, a page outside [0, n_pages) is never read or
+ * written (its keys are left out), a row with more new tokens before it than kv_len allows
+ * sees no key.  Rows of Q behind q_start[n_seq] are not read, theirs of O left as they were.
+ * The rows of slots [0, kv_len) must be finite (pages behind that are never read).
+ * Sequences may share pages that are only read; a page that a call writes (append, evict,
+ * weights) must be in one place of one sequence's table.
+ * Limits: D in {64, 128}; n_seq <= 65535; T H_q / H_kv < 2^31; max_pages page_size <= 2^30;
+ * the pages of one K or V head must span less than 64 GiB. */
+typedef struct {
+    int64_t T;                /* new tokens of all sequences: rows of Q, O, new K and V    */
+    int32_t n_seq;
+    int32_t H_q, H_kv, D;
+    int32_t dtype;            /* dhsa_dtype of Q, K, V and O                               */
+    int32_t page_size;        /* slots of a page, >= 1                                     */
+    int32_t n_pages;          /* pages of the pool                                         */
+    int32_t max_pages;        /* pages of a sequence: row length of the table              */
+    float scale;              /* softmax scale; 0 means 1/sqrt(D)                          */
+    int64_t window;           /* 0: a token at slot i attends to all slots j <= i; > 0: to
+                                 those with i - j < window or j < sinks                    */
+    int64_t sinks;
+    int64_t q_stride_h, q_stride_t;   /* Q [H_q][T][D], in elements; 0 = packed              */
+    int64_t o_stride_h, o_stride_t;
+    int64_t k_stride_p, k_stride_h, k_stride_s;   /* page, kv-head, slot; 0 = packed        */
+    int64_t v_stride_p, v_stride_h, v_stride_s;
+    int64_t kn_stride_h, kn_stride_t;  /* new K and V [H_kv][T][D] (dhsa_paged_append)       */
+    int64_t vn_stride_h, vn_stride_t;
+} dhsa_paged;
+
+/* New rows into the cache: row t of sequence s goes to slot kv_len[s] - n_s + (t - q_start[s]).
+ * weights_dev (may be NULL): set to 0 for those slots (see dhsa_paged_attend). */
+dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, const void *V_new_dev, void *K_dev,
+                              void *V_dev, const int32_t *table_dev, const int32_t *q_start_dev,
+                              const int32_t *kv_len_dev, float *weights_dev, void *stream);
+
+/* Attention of the new tokens over the cache, their own rows included (append them first).
+ * lse_dev (may be NULL): float [H_q][T], log of the sum of exp(q . k scale) over the row's
+ * keys.  A row without keys gets O = 0 and lse = -infinity.
+ * weights_dev (may be NULL): float [n_pages][H_kv][page_size], what each cached key has got of
+ * attention: for every slot of the call's sequences
+ *   weights = decay weights + sum over the call's rows and the query heads of the kv-head of
+ *             exp(q . k scale - lse)
+ * (decay in [0, 1]; with 0 the old values are not read; else DHSA_ERR_SHAPE).  The sums are made in a fixed order.
+ * ws_dev: scratch of dhsa_paged_workspace_bytes(prob) bytes, 16-byte aligned, nothing in which
+ * has to be set; calls that share it must be ordered.  The size depends on T, n_seq and the
+ * head counts only. */
+dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev, const void *K_dev, const void *V_dev,
+                              const int32_t *table_dev, const int32_t *q_start_dev, const int32_t *kv_len_dev,
+                              void *O_dev, float *lse_dev, float *weights_dev, float decay, void *ws_dev,
+                              size_t ws_bytes, void *stream);
+size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob);   /* 0 on invalid arguments */
+
+/* Every sequence of more than `keep` tokens is cut down to `keep`: of each kv-head the slots
+ * [0, first) and the last `recent` stay, and of the others those with the largest weights (equal
+ * ones: lower slots; a NaN counts as less than any number).  What stays keeps its order and moves
+ * to the slots 0 .. keep - 1 of table_out_dev: K, V and weights.  table_out_dev: table_dev itself
+ * (in place; slots behind are left as they were) or a table of the same shape whose pages are
+ * not in table_dev (the old pages are left as they were; shorter sequences move whole).  T, Q and
+ * window play no part.  kv_len_out_dev: int32 [n_seq], min(kv_len, keep); may be kv_len_dev.
+ * idx_dev (may be NULL): int32 [n_seq][H_kv][keep], the slots that stayed, ascending, -1 behind.
+ * keep >= 1, first >= 0, recent >= 0, first + recent <= keep (else DHSA_ERR_BUDGET).  K rows are
+ * moved as they are: a rotary position stays the token's own, while a window counts slots.
+ * ws_dev: scratch of dhsa_paged_evict_workspace_bytes(prob, keep) bytes, as above. */
+dhsa_status dhsa_paged_evict(const dhsa_paged *prob, void *K_dev, void *V_dev, float *weights_dev,
+                             const int32_t *table_dev, const int32_t *kv_len_dev, int32_t keep, int32_t first,
+                             int32_t recent, const int32_t *table_out_dev, int32_t *kv_len_out_dev,
+                             int32_t *idx_dev, void *ws_dev, size_t ws_bytes, void *stream);
+size_t dhsa_paged_evict_workspace_bytes(const dhsa_paged *prob, int32_t keep);
+
 const char *dhsa_status_string(dhsa_status s);
-int dhsa_version(void);   /* 201: counters in the decoding workspace lie in front of what depends on the budget */
+int dhsa_version(void);   /* 202: windows and paged caches */
 
 #ifdef __cplusplus
 }

@@ -33,6 +33,8 @@ EXPORTS = ["dhsa_plan_bytes", "dhsa_workspace_bytes", "dhsa_route", "dhsa_sparse
            "dhsa_finalize_boundaries", "dhsa_finalize_boundaries_workspace_bytes",
            "dhsa_recall_rows", "dhsa_recall_workspace_bytes",
            "dhsa_decode_step", "dhsa_decode_workspace_bytes",
+           "dhsa_window_prefill", "dhsa_paged_append", "dhsa_paged_attend", "dhsa_paged_workspace_bytes",
+           "dhsa_paged_evict", "dhsa_paged_evict_workspace_bytes",
            "dhsa_status_string", "dhsa_version"]
 
 
@@ -47,6 +49,16 @@ class dhsa_problem(C.Structure):
                 ("v_stride_h", C.c_int64), ("v_stride_l", C.c_int64),
                 ("o_stride_h", C.c_int64), ("o_stride_l", C.c_int64),
                 ("B_r", C.c_int32), ("pooling", C.c_int32)]
+
+
+class dhsa_paged(C.Structure):
+    _fields_ = [("T", C.c_int64), ("n_seq", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("D", C.c_int32),
+                ("dtype", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("scale", C.c_float), ("window", C.c_int64), ("sinks", C.c_int64),
+                ("q_stride_h", C.c_int64), ("q_stride_t", C.c_int64), ("o_stride_h", C.c_int64), ("o_stride_t", C.c_int64),
+                ("k_stride_p", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_s", C.c_int64),
+                ("v_stride_p", C.c_int64), ("v_stride_h", C.c_int64), ("v_stride_s", C.c_int64),
+                ("kn_stride_h", C.c_int64), ("kn_stride_t", C.c_int64), ("vn_stride_h", C.c_int64), ("vn_stride_t", C.c_int64)]
 
 
 class DhsaError(RuntimeError):
@@ -105,6 +117,16 @@ def lib() -> C.CDLL:
         l.dhsa_decode_step.restype = C.c_int
         l.dhsa_decode_workspace_bytes.argtypes = [P, C.c_int32, C.c_int64]
         l.dhsa_decode_workspace_bytes.restype = C.c_size_t
+        G = C.POINTER(dhsa_paged)
+        l.dhsa_window_prefill.argtypes = [P, C.c_int64, C.c_int64, vp, vp, vp, vp, vp]
+        l.dhsa_window_prefill.restype = C.c_int
+        l.dhsa_paged_append.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp]; l.dhsa_paged_append.restype = C.c_int
+        l.dhsa_paged_attend.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
+        l.dhsa_paged_attend.restype = C.c_int
+        l.dhsa_paged_workspace_bytes.argtypes = [G]; l.dhsa_paged_workspace_bytes.restype = C.c_size_t
+        l.dhsa_paged_evict.argtypes = [G, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_size_t, vp]
+        l.dhsa_paged_evict.restype = C.c_int
+        l.dhsa_paged_evict_workspace_bytes.argtypes = [G, C.c_int32]; l.dhsa_paged_evict_workspace_bytes.restype = C.c_size_t
         l.dhsa_status_string.argtypes = [C.c_int]; l.dhsa_status_string.restype = C.c_char_p
         l.dhsa_version.argtypes = []; l.dhsa_version.restype = C.c_int
         _lib = l
@@ -342,6 +364,119 @@ def dhsa_decode_step(prob, Q, K, V, B, ws, N_c_cap: int, L_cap: int, kc_valid: i
                                   kc_valid, O_row.data_ptr(), idx.data_ptr() if want_idx else None,
                                   cnt.data_ptr() if want_idx else None, ws.data_ptr(), ws.numel(), _stream()))
     return (O_row, idx, cnt) if want_idx else O_row
+
+
+# ---- attention without routing: windows and paged caches ----
+
+def _same(what: str, t, dtype, shape, contiguous: bool = False) -> None:
+    """The tensors of the calls below are described by one problem struct: what does not fit it is refused here."""
+    if t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, where {dtype} {shape} on the current device is wanted")
+    if not (t.is_contiguous() if contiguous else t.stride(-1) == 1 and 0 not in t.stride()):   # (a stride of 0 says packed)
+        raise ValueError(f"{what}: strides {t.stride()}: contiguous rows are wanted, none of them shared")
+
+
+def dhsa_window_prefill(prob, Q, K, V, O, window: int, sinks: int = 0) -> None:
+    """Causal attention of a prompt in which row i sees the keys j <= i with i - j < window or j < sinks.  prob: problem(Q, K,
+    [0, L], L); its chunks and budget play no part."""
+    kv = (prob.H_kv, prob.L, prob.D)
+    _same("Q", Q, Q.dtype, (prob.H_q, prob.L, prob.D)); _same("O", O, Q.dtype, (prob.H_q, prob.L, prob.D))
+    _same("K", K, Q.dtype, kv); _same("V", V, Q.dtype, kv)
+    p = _with_vo(prob, V, O)
+    _check(lib().dhsa_window_prefill(C.byref(p), window, sinks, Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                                     _stream()))
+
+
+def paged_problem(K, V, table, H_q: int, T: int, window: int = 0, sinks: int = 0, scale: float = 0.0) -> dhsa_paged:
+    """Describe a pool of pages K, V [n_pages, H_kv, page_size, D] (any strides, last dim contiguous), the page table [n_seq,
+    max_pages] and the T new tokens of a call.  A contiguous cache [H_kv, L, D] is K[None], one page of L slots."""
+    n_pages, H_kv, page_size, D = K.shape
+    p = dhsa_paged(T, table.shape[0], H_q, H_kv, D, _DTYPES.get(K.dtype, -1), page_size, n_pages, table.shape[1], scale, window, sinks)
+    p.k_stride_p, p.k_stride_h, p.k_stride_s = K.stride()[:3]
+    p.v_stride_p, p.v_stride_h, p.v_stride_s = V.stride()[:3]
+    return p
+
+
+def dhsa_paged_workspace_bytes(prob: dhsa_paged) -> int:
+    return int(lib().dhsa_paged_workspace_bytes(C.byref(prob)))
+
+
+def dhsa_paged_evict_workspace_bytes(prob: dhsa_paged, keep: int) -> int:
+    return int(lib().dhsa_paged_evict_workspace_bytes(C.byref(prob), keep))
+
+
+def alloc_paged(prob: dhsa_paged, device="cuda"):
+    """Workspace of dhsa_paged_attend: of a problem with as many new tokens and sequences, whatever their lengths."""
+    n = dhsa_paged_workspace_bytes(prob)
+    if n == 0:
+        raise DhsaError(2, "problem rejected by dhsa_paged_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_evict(prob: dhsa_paged, keep: int, device="cuda"):
+    """Workspace of dhsa_paged_evict."""
+    n = dhsa_paged_evict_workspace_bytes(prob, keep)
+    if n == 0:
+        raise DhsaError(2, "problem or budget rejected by dhsa_paged_evict_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _same_cache(prob, K, V, table, weights) -> None:
+    pool = (prob.n_pages, prob.H_kv, prob.page_size, prob.D)
+    _same("K", K, K.dtype, pool); _same("V", V, K.dtype, pool)
+    if _DTYPES.get(K.dtype, -1) != prob.dtype or K.stride()[:3] != (prob.k_stride_p, prob.k_stride_h, prob.k_stride_s) or \
+            V.stride()[:3] != (prob.v_stride_p, prob.v_stride_h, prob.v_stride_s):
+        raise ValueError("K and V are not laid out as the problem says")
+    _same("table", table, torch.int32, (prob.n_seq, prob.max_pages), True)
+    if weights is not None:
+        _same("weights", weights, torch.float32, pool[:3], True)
+
+
+def dhsa_paged_append(prob, K_new, V_new, K, V, table, q_start, kv_len, weights=None) -> None:
+    """New rows K_new, V_new [H_kv, T, D] into the slots kv_len[s] - n_s .. kv_len[s] - 1 of their sequences; `weights` (float
+    [n_pages, H_kv, page_size]) becomes 0 there."""
+    _same_cache(prob, K, V, table, weights)
+    new = (prob.H_kv, prob.T, prob.D)
+    _same("K_new", K_new, K.dtype, new); _same("V_new", V_new, K.dtype, new)
+    _same("q_start", q_start, torch.int32, (prob.n_seq + 1,), True); _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True)
+    p = dhsa_paged.from_buffer_copy(prob)
+    p.kn_stride_h, p.kn_stride_t = K_new.stride()[:2]
+    p.vn_stride_h, p.vn_stride_t = V_new.stride()[:2]
+    _check(lib().dhsa_paged_append(C.byref(p), K_new.data_ptr(), V_new.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(),
+                                   q_start.data_ptr(), kv_len.data_ptr(), None if weights is None else weights.data_ptr(),
+                                   _stream()))
+
+
+def dhsa_paged_attend(prob, Q, K, V, table, q_start, kv_len, O, ws, lse=None, weights=None, decay: float = 1.0) -> None:
+    """Attention of the new tokens Q [H_q, T, D] over the cache, their own rows included: O like Q, lse float [H_q, T].
+    weights (float [n_pages, H_kv, page_size]) = decay weights + what each cached key got from this call's rows and heads."""
+    _same_cache(prob, K, V, table, weights)
+    rows = (prob.H_q, prob.T, prob.D)
+    _same("Q", Q, K.dtype, rows); _same("O", O, K.dtype, rows)
+    _same("q_start", q_start, torch.int32, (prob.n_seq + 1,), True); _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True)
+    if lse is not None:
+        _same("lse", lse, torch.float32, rows[:2], True)
+    p = dhsa_paged.from_buffer_copy(prob)
+    p.q_stride_h, p.q_stride_t = Q.stride()[:2]
+    p.o_stride_h, p.o_stride_t = O.stride()[:2]
+    _check(lib().dhsa_paged_attend(C.byref(p), Q.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(), q_start.data_ptr(),
+                                   kv_len.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(),
+                                   None if weights is None else weights.data_ptr(), decay, ws.data_ptr(), ws.numel(), _stream()))
+
+
+def dhsa_paged_evict(prob, K, V, weights, table, kv_len, keep: int, first: int, recent: int, ws, kv_len_out, table_out=None,
+                     idx=None) -> None:
+    """Cut every sequence down to `keep` tokens: of each kv-head the first ones, the `recent` last ones and the heaviest others
+    stay and move to the front, in place or into the pages of table_out.  idx: int32 [n_seq, H_kv, keep], the slots that stayed."""
+    _same_cache(prob, K, V, table, weights)
+    _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True); _same("kv_len_out", kv_len_out, torch.int32, (prob.n_seq,), True)
+    if table_out is not None:
+        _same("table_out", table_out, torch.int32, (prob.n_seq, prob.max_pages), True)
+    if idx is not None:
+        _same("idx", idx, torch.int32, (prob.n_seq, prob.H_kv, keep), True)
+    _check(lib().dhsa_paged_evict(C.byref(prob), K.data_ptr(), V.data_ptr(), weights.data_ptr(), table.data_ptr(), kv_len.data_ptr(),
+                                  keep, first, recent, (table if table_out is None else table_out).data_ptr(), kv_len_out.data_ptr(),
+                                  None if idx is None else idx.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
 
 
 def dhsa_version() -> int:

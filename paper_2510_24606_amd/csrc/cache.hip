@@ -1,0 +1,200 @@
+// A paged cache written and cut down: dhsa_paged_append, dhsa_paged_evict.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace dhsa {
+
+// ---------------------------------------------------------------------------
+// Append: a workgroup per new token moves its rows of all kv-heads, 16 bytes a thread.  Bound by a chain of three loads (the
+// sequence of the token, its length, the page) where tokens are few, by the copy where they are many.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_append(SpanArgs a, AppendArgs ap, int row16, int t0) {
+    const int t = t0 + blockIdx.x, lane = threadIdx.x & 63;
+    int s = 0;                                        // sequences that end at or before the token
+    for (int s0 = 0; s0 < a.n_seq; s0 += 64) s += __popcll(__ballot(s0 + lane < a.n_seq && a.q_start[s0 + lane + 1] <= t));
+    if (s >= a.n_seq) return;
+    const Seq q = read_seq(a, s);
+    const int slot = q.kv - q.n + (t - (int)q.q0);
+    if (t < q.q0 || t >= q.q0 + q.n || slot < 0) return;
+    const int pi = page_of(a, slot), in = slot - pi * a.page_size, page = a.table[(int64_t)s * a.max_pages + pi];
+    if ((unsigned)page >= (unsigned)a.n_pages) return;
+    const int64_t kd = (int64_t)((uint64_t)((uint32_t)page * a.ks_p + (uint32_t)in * a.ks_s) << 4);
+    const int64_t vd = (int64_t)((uint64_t)((uint32_t)page * a.vs_p + (uint32_t)in * a.vs_s) << 4);
+    for (int x = threadIdx.x; x < a.H_kv * row16; x += 256) {
+        const int g = x / row16, c = 16 * (x % row16);
+        const uint4 k = *reinterpret_cast<const uint4 *>(ap.Kn + g * ap.kns_h + t * ap.kns_t + c);
+        const uint4 v = *reinterpret_cast<const uint4 *>(ap.Vn + g * ap.vns_h + t * ap.vns_t + c);
+        *reinterpret_cast<uint4 *>(ap.K + g * a.ks_h + kd + c) = k;
+        *reinterpret_cast<uint4 *>(ap.V + g * a.vs_h + vd + c) = v;
+    }
+    if (ap.weights)
+        for (int g = threadIdx.x; g < a.H_kv; g += 256) ap.weights[((int64_t)page * a.H_kv + g) * a.page_size + in] = 0.f;
+}
+
+hipError_t launch_append(const SpanArgs &a, const AppendArgs &ap, int row_bytes, hipStream_t s) {
+    hipError_t e = hipSuccess;
+    for (int64_t t0 = 0; t0 < a.T && e == hipSuccess; t0 += kGridMax) {
+        hipLaunchKernelGGL(k_append, dim3((unsigned)std::min<int64_t>(a.T - t0, kGridMax)), dim3(256), 0, s, a, ap, row_bytes / 16, (int)t0);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// ---------------------------------------------------------------------------
+// Eviction, first launch: which slots stay.  A workgroup per sequence and kv-head.  The middle slots [first, kv - recent) are
+// ordered by a 32-bit key of their weight; the key of the last one that stays is found digit by digit (counts in LDS), then
+// the slots above it, and of those equal to it the first ones, are listed in order.
+// ---------------------------------------------------------------------------
+// larger weight, larger key; -0 = 0; NaN and slots without a page: 0, less than any number
+__device__ __forceinline__ uint32_t weight_key(float w) {
+    if (w != w) return 0u;
+    const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+
+__global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, EvictArgs e) {
+    __shared__ int hist[2048];
+    __shared__ int s_gt[kEvictWaves], s_eq[kEvictWaves], s_scan[kEvictWaves];
+    __shared__ int s_digit, s_left;
+    const int g = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int kv = a.kv_len[s];
+    kv = kv < 0 ? 0 : kv > a.slots_max ? a.slots_max : kv;
+    const int64_t at = (int64_t)s * a.H_kv + g;
+    int32_t *list = e.list + at * e.stride, *idx = e.idx ? e.idx + at * e.keep : nullptr;
+    const int n = kv < e.keep ? kv : e.keep;
+    if (tid == 0) e.count[at] = n;
+    for (int x = n + tid; idx && x < e.keep; x += kEvictThreads) idx[x] = -1;
+    const auto put = [&](int x, int slot) { list[x] = slot; if (idx) idx[x] = slot; };
+    if (kv <= e.keep) {
+        for (int x = tid; x < n; x += kEvictThreads) put(x, x);
+        return;
+    }
+    const int m0 = e.first, m1 = kv - e.recent, need = e.keep - e.first - e.recent;
+    for (int x = tid; x < e.first; x += kEvictThreads) put(x, x);
+    for (int x = tid; x < e.recent; x += kEvictThreads) put(e.keep - e.recent + x, m1 + x);
+    if (need == 0) return;
+    const int32_t *table = a.table + (int64_t)s * a.max_pages;
+    const auto key = [&](int slot) {
+        const int pi = page_of(a, slot), page = table[pi];
+        if ((unsigned)page >= (unsigned)a.n_pages) return 0u;
+        return weight_key(e.weights[((int64_t)page * a.H_kv + g) * a.page_size + (slot - pi * a.page_size)]);
+    };
+    // digits of 11, 11 and 10 bits
+    uint32_t prefix = 0;
+    int left = need;             // of the slots whose higher digits equal the prefix, how many stay
+    for (int d = 0; d < 3; ++d) {
+        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
+        for (int x = tid; x < 2048; x += kEvictThreads) hist[x] = 0;
+        __syncthreads();
+        for (int x = m0 + tid; x < m1; x += kEvictThreads) {
+            const uint32_t k = key(x);
+            if (d == 0 || k >> (shift + (d == 1 ? 11 : 10)) == prefix) atomicAdd(&hist[k >> shift & (bins - 1)], 1);
+        }
+        __syncthreads();
+        // thread i has the bins 2047 - 2 i and 2046 - 2 i: counts from the top down
+        const int h1 = hist[2047 - 2 * tid], h0 = hist[2046 - 2 * tid];
+        const int inc = wave_incl_scan(h0 + h1);
+        if (lane == 63) s_scan[wave] = inc;
+        __syncthreads();
+        int above = inc - h0 - h1;
+        for (int w = 0; w < wave; ++w) above += s_scan[w];
+        if (above < left && left <= above + h1) { s_digit = 2047 - 2 * tid; s_left = left - above; }
+        else if (above + h1 < left && left <= above + h1 + h0) { s_digit = 2046 - 2 * tid; s_left = left - above - h1; }
+        __syncthreads();
+        prefix = prefix << (d == 2 ? 10 : 11) | (uint32_t)s_digit;
+        left = s_left;
+    }
+    // the list: a wave has consecutive slots
+    const int len = m1 - m0, per = (len + kEvictThreads - 1) / kEvictThreads * 64;
+    const int w0 = m0 + wave * per, w1 = w0 + per < m1 ? w0 + per : m1;
+    int gt = 0, eq = 0;
+    for (int x = w0 + lane; x < w1; x += 64) {
+        const uint32_t k = key(x);
+        gt += k > prefix;
+        eq += k == prefix;
+    }
+    gt = __builtin_amdgcn_readlane(wave_incl_scan(gt), 63);
+    eq = __builtin_amdgcn_readlane(wave_incl_scan(eq), 63);
+    if (lane == 0) { s_gt[wave] = gt; s_eq[wave] = eq; }
+    __syncthreads();
+    int gt0 = 0, eq0 = 0;        // above and equal in the slots before
+    for (int w = 0; w < wave; ++w) { gt0 += s_gt[w]; eq0 += s_eq[w]; }
+    for (int x0 = w0; x0 < w1; x0 += 64) {
+        const int x = x0 + lane;
+        const uint32_t k = x < w1 ? key(x) : 0u;
+        const unsigned long long mg = __ballot(x < w1 && k > prefix), me = __ballot(x < w1 && k == prefix);
+        const unsigned long long below = (1ull << lane) - 1ull;
+        const int ge = gt0 + __popcll(mg & below), ee = eq0 + __popcll(me & below);
+        if (x < w1 && (k > prefix || (k == prefix && ee < left))) put(e.first + ge + (ee < left ? ee : left), x);
+        gt0 += __popcll(mg);
+        eq0 += __popcll(me);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Eviction, second launch: the rows move.  Kept slots ascend, so row t moves from a slot >= t; batches are read whole before
+// they are written, and a batch is written below everything that a later one reads: a workgroup does its columns of a head
+// in place.  blockIdx.x: part (K columns, V columns, weights), y: kv-head, z: sequence.
+// ---------------------------------------------------------------------------
+constexpr int kMoveU = 4;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+template <typename V>
+__device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e, int s, int n, const int32_t *list, char *base, uint64_t p16,
+                                          uint64_t s16, int unit, int lanes, int width) {
+    // lanes threads per row, width bytes each; strides in `unit` bytes
+    const int tid = threadIdx.x, r = tid / lanes, c = tid % lanes * width, rows = kEvictThreads / lanes;
+    const int32_t *table = a.table + (int64_t)s * a.max_pages, *table_out = e.table_out + (int64_t)s * a.max_pages;
+    const auto place = [&](const int32_t *tb, int slot) -> char * {
+        const int pi = page_of(a, slot), page = tb[pi];
+        if ((unsigned)page >= (unsigned)a.n_pages) return nullptr;
+        return base + ((uint64_t)page * p16 + (uint64_t)(slot - pi * a.page_size) * s16) * unit + c;
+    };
+    for (int t0 = 0; t0 < n; t0 += rows * kMoveU) {
+        V x[kMoveU];
+        char *to[kMoveU];
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u) {
+            const int t = t0 + u * rows + r;
+            to[u] = nullptr;
+            x[u] = V{};
+            if (t < n && !(table == table_out && list[t] == t)) {
+                const char *from = place(table, list[t]);
+                if (from) { x[u] = *reinterpret_cast<const V *>(from); to[u] = place(table_out, t); }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u)
+            if (to[u]) *reinterpret_cast<V *>(to[u]) = x[u];
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kEvictThreads) void k_evict_move(SpanArgs a, EvictArgs e, int row16, int parts) {
+    const int g = blockIdx.y, s = blockIdx.z, part = blockIdx.x;
+    const int64_t at = (int64_t)s * a.H_kv + g;
+    const int n = e.count[at];
+    const int32_t *list = e.list + at * e.stride;
+    if (part == 2 * parts) {
+        move_rows<float>(a, e, s, n, list, (char *)(e.weights + (int64_t)g * a.page_size), (uint64_t)a.H_kv * a.page_size, 1, 4, 1, 4);
+        if (g == 0 && threadIdx.x == 0) e.kv_out[s] = n;      // (nothing of this launch reads kv_len)
+        return;
+    }
+    const bool is_k = part < parts;
+    const int lanes = row16 / parts, c0 = (is_k ? part : part - parts) * lanes * 16;
+    move_rows<u32x4_t>(a, e, s, n, list, (is_k ? e.K + g * a.ks_h : e.V + g * a.vs_h) + c0, is_k ? a.ks_p : a.vs_p, is_k ? a.ks_s : a.vs_s, 16,
+                     lanes, 16);
+}
+
+hipError_t launch_evict(const SpanArgs &a, const EvictArgs &e, int row_bytes, hipStream_t s) {
+    const int row16 = row_bytes / 16, parts = row16 / 8;      // 128 bytes a part
+    hipLaunchKernelGGL(k_evict_select, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
+    hipLaunchKernelGGL(k_evict_move, dim3(2 * parts + 1, a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e, row16, parts);
+    return hipGetLastError();
+}
+
+}  // namespace dhsa

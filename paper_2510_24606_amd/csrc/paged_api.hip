@@ -1,0 +1,220 @@
+// Host side of the entry points without routing (windows, paged caches): argument checks, workspace layout, launches.
+// See include/dhsa.h for the contract of every one.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "paged.h"
+
+using namespace dhsa;
+
+namespace {
+
+#define DHSA_API __attribute__((visibility("default")))
+
+bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+
+// slot / page_size as a multiplication: with l = ceil(log2 d) and mul = floor(2^(31 + l) / d) + 1 < 2^32, mul d - 2^(31 + l) is
+// in 1 .. d <= 2^l, so x mul / 2^(31 + l) is above x / d by less than 1 / d for x < 2^31
+void set_divisor(uint32_t d, SpanArgs *a) {
+    int l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    a->div_mul = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
+    a->div_shift = 31 + l;
+}
+
+// What the two problem structs have in common.
+dhsa_status heads(int64_t H_q, int64_t H_kv, int32_t D, int32_t dtype, float scale, SpanArgs *a) {
+    if (dtype != DHSA_F32 && dtype != DHSA_BF16) return DHSA_ERR_DTYPE;
+    if (H_q < 1 || H_kv < 1 || H_q % H_kv != 0 || H_q > 65535 - H_kv) return DHSA_ERR_SHAPE;
+    if (D != 64 && D != 128) return DHSA_ERR_SHAPE;
+    if (!(scale >= 0.f) || !isfinite(scale)) return DHSA_ERR_SHAPE;
+    *a = SpanArgs{};
+    a->H_kv = (int)H_kv;
+    a->G = (int)(H_q / H_kv);
+    a->scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    return DHSA_OK;
+}
+
+// A stride in elements: the default where it is 0, at least `least`, a multiple of 16 bytes.
+dhsa_status stride(int64_t in, int64_t packed, int64_t least, int esz, int64_t *out) {
+    *out = in ? in : packed;
+    if (*out < least || *out > INT64_MAX / 64) return DHSA_ERR_SHAPE;
+    return (*out * esz) % 16 != 0 ? DHSA_ERR_ALIGN : DHSA_OK;
+}
+
+// Do n rows of `step` elements' distance, behind m of `far`, end within 64 GiB?
+bool fits(int64_t n, int64_t step, int64_t m, int64_t far, int D, int esz) {
+    const __int128 last = (__int128)(n - 1) * step + (__int128)(m - 1) * far + D;
+    return last * esz < (__int128)1 << 36;
+}
+
+dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
+    if (!in) return DHSA_ERR_NULL;
+    dhsa_status st = heads(in->H_q, in->H_kv, in->D, in->dtype, in->scale, a);
+    if (st != DHSA_OK) return st;
+    if (in->n_seq < 0 || in->n_seq > 65535 || in->T < 0 || in->T > INT_MAX / a->G) return DHSA_ERR_SHAPE;
+    if (in->page_size < 1 || in->n_pages < 1 || in->max_pages < 1) return DHSA_ERR_SHAPE;
+    if ((int64_t)in->page_size * in->max_pages > (int64_t)1 << 30) return DHSA_ERR_SHAPE;
+    if (in->window < 0 || in->sinks < 0) return DHSA_ERR_SHAPE;
+    const int esz = in->dtype == DHSA_F32 ? 4 : 2;
+    const int64_t D = in->D, T = in->T, ps = in->page_size, H_kv = in->H_kv;
+    int64_t ks_p, ks_h, ks_s, vs_p, vs_h, vs_s, kn_h, kn_t, vn_h, vn_t;
+    const struct { int64_t in, packed, least; int64_t *out; } all[] = {
+        {in->q_stride_h, std::max<int64_t>(T, 1) * D, 0, &a->qs_h}, {in->q_stride_t, D, D, &a->qs_t},
+        {in->o_stride_h, std::max<int64_t>(T, 1) * D, 0, &a->os_h}, {in->o_stride_t, D, D, &a->os_t},
+        {in->k_stride_p, H_kv * ps * D, D, &ks_p}, {in->k_stride_h, ps * D, 0, &ks_h}, {in->k_stride_s, D, D, &ks_s},
+        {in->v_stride_p, H_kv * ps * D, D, &vs_p}, {in->v_stride_h, ps * D, 0, &vs_h}, {in->v_stride_s, D, D, &vs_s},
+        {in->kn_stride_h, std::max<int64_t>(T, 1) * D, 0, &kn_h}, {in->kn_stride_t, D, D, &kn_t},
+        {in->vn_stride_h, std::max<int64_t>(T, 1) * D, 0, &vn_h}, {in->vn_stride_t, D, D, &vn_t}};
+    for (const auto &x : all)
+        if ((st = stride(x.in, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
+    if (!fits(in->n_pages, ks_p, ps, ks_s, in->D, esz) || !fits(in->n_pages, vs_p, ps, vs_s, in->D, esz)) return DHSA_ERR_SHAPE;
+    a->T = T;
+    a->n_seq = in->n_seq;
+    a->n_pages = in->n_pages; a->max_pages = in->max_pages; a->page_size = in->page_size;
+    a->slots_max = in->page_size * in->max_pages;
+    set_divisor((uint32_t)in->page_size, a);
+    a->window = in->window == 0 || in->window > INT_MAX ? INT_MAX : (int)in->window;
+    a->sinks = (int)std::min<int64_t>(in->sinks, INT_MAX);
+    // (a stride of a single page or slot is not used and may not fit)
+    a->ks_p = in->n_pages > 1 ? (uint32_t)(ks_p * esz / 16) : 0; a->ks_s = ps > 1 ? (uint32_t)(ks_s * esz / 16) : 0;
+    a->vs_p = in->n_pages > 1 ? (uint32_t)(vs_p * esz / 16) : 0; a->vs_s = ps > 1 ? (uint32_t)(vs_s * esz / 16) : 0;
+    a->ks_h = ks_h * esz; a->vs_h = vs_h * esz;
+    if (ap) { ap->kns_h = kn_h * esz; ap->kns_t = kn_t * esz; ap->vns_h = vn_h * esz; ap->vns_t = vn_t * esz; }
+    return DHSA_OK;
+}
+
+// Workspace of dhsa_paged_attend in bytes.
+struct PagedWs { int64_t off_info, off_state, off_part, off_norm, bytes; };
+PagedWs paged_ws(SpanArgs *a, int D, int dtype) {
+    a->target = (int)span_target(*a, dtype);
+    const int64_t M = span_rows(*a, dtype);
+    a->part_cap = a->target > 0 ? 2 * a->target + a->H_kv : 0;
+    PagedWs w;
+    w.off_info = 256;
+    w.off_state = w.off_info + up256((int64_t)a->part_cap * 16);
+    w.off_part = w.off_state + up256((int64_t)a->part_cap * M * 8);
+    w.off_norm = w.off_part + up256((int64_t)a->part_cap * M * D * 4);
+    w.bytes = w.off_norm + up256(a->T * a->H_kv * a->G * 8);
+    return w;
+}
+
+dhsa_status hip_status(hipError_t e) { return e == hipSuccess ? DHSA_OK : DHSA_ERR_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+DHSA_API dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t window, int64_t sinks, const void *Q_dev,
+                                         const void *K_dev, const void *V_dev, void *O_dev, void *stream) {
+    if (!prob) return DHSA_ERR_NULL;
+    SpanArgs a;
+    dhsa_status st = heads(prob->H_q, prob->H_kv, prob->D, prob->dtype, prob->scale, &a);
+    if (st != DHSA_OK) return st;
+    if (prob->L < 1 || prob->L > INT_MAX / a.G || window < 1 || sinks < 0) return DHSA_ERR_SHAPE;
+    const int esz = prob->dtype == DHSA_F32 ? 4 : 2;
+    const int64_t D = prob->D, L = prob->L;
+    int64_t ks_h, ks_l, vs_h, vs_l;
+    const struct { int64_t in, packed, least; int64_t *out; } all[] = {
+        {prob->q_stride_h, L * D, 0, &a.qs_h}, {prob->q_stride_l, D, D, &a.qs_t}, {prob->k_stride_h, L * D, 0, &ks_h},
+        {prob->k_stride_l, D, D, &ks_l}, {prob->v_stride_h, L * D, 0, &vs_h}, {prob->v_stride_l, D, D, &vs_l},
+        {prob->o_stride_h, L * D, 0, &a.os_h}, {prob->o_stride_l, D, D, &a.os_t}};
+    for (const auto &x : all)
+        if ((st = stride(x.in, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
+    if (!fits(L, ks_l, 1, 0, prob->D, esz) || !fits(L, vs_l, 1, 0, prob->D, esz)) return DHSA_ERR_SHAPE;
+    if (!Q_dev || !K_dev || !V_dev || !O_dev) return DHSA_ERR_NULL;
+    if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev)) return DHSA_ERR_ALIGN;
+    a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev;
+    a.T = L; a.n_seq = 1;
+    a.window = window > INT_MAX ? INT_MAX : (int)window;
+    a.sinks = (int)std::min<int64_t>(sinks, INT_MAX);
+    a.ks_s = L > 1 ? (uint32_t)(ks_l * esz / 16) : 0; a.vs_s = L > 1 ? (uint32_t)(vs_l * esz / 16) : 0;
+    a.ks_h = ks_h * esz; a.vs_h = vs_h * esz;
+    return hip_status(launch_span(a, prob->D, prob->dtype, static_cast<hipStream_t>(stream)));
+}
+
+DHSA_API dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, const void *V_new_dev, void *K_dev,
+                                       void *V_dev, const int32_t *table_dev, const int32_t *q_start_dev,
+                                       const int32_t *kv_len_dev, float *weights_dev, void *stream) {
+    SpanArgs a;
+    AppendArgs ap;
+    const dhsa_status st = resolve_paged(prob, &a, &ap);
+    if (st != DHSA_OK) return st;
+    if (a.n_seq == 0 || a.T == 0) return DHSA_OK;
+    if (!K_new_dev || !V_new_dev || !K_dev || !V_dev || !table_dev || !q_start_dev || !kv_len_dev) return DHSA_ERR_NULL;
+    if (misaligned(K_new_dev) || misaligned(V_new_dev) || misaligned(K_dev) || misaligned(V_dev)) return DHSA_ERR_ALIGN;
+    a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev;
+    ap.Kn = (const char *)K_new_dev; ap.Vn = (const char *)V_new_dev; ap.K = (char *)K_dev; ap.V = (char *)V_dev;
+    ap.weights = weights_dev;
+    return hip_status(launch_append(a, ap, prob->D * (prob->dtype == DHSA_F32 ? 4 : 2), static_cast<hipStream_t>(stream)));
+}
+
+DHSA_API size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob) {
+    SpanArgs a;
+    if (resolve_paged(prob, &a, nullptr) != DHSA_OK) return 0;
+    return (size_t)paged_ws(&a, prob->D, prob->dtype).bytes;
+}
+
+DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev, const void *K_dev, const void *V_dev,
+                                       const int32_t *table_dev, const int32_t *q_start_dev, const int32_t *kv_len_dev,
+                                       void *O_dev, float *lse_dev, float *weights_dev, float decay, void *ws_dev,
+                                       size_t ws_bytes, void *stream) {
+    SpanArgs a;
+    const dhsa_status st = resolve_paged(prob, &a, nullptr);
+    if (st != DHSA_OK) return st;
+    if (!(decay >= 0.f && decay <= 1.f)) return DHSA_ERR_SHAPE;
+    if (a.n_seq == 0 || (a.T == 0 && !weights_dev)) return DHSA_OK;
+    if ((a.T > 0 && (!Q_dev || !O_dev)) || !K_dev || !V_dev || !table_dev || !q_start_dev || !kv_len_dev || !ws_dev)
+        return DHSA_ERR_NULL;
+    if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(ws_dev)) return DHSA_ERR_ALIGN;
+    const PagedWs w = paged_ws(&a, prob->D, prob->dtype);
+    if (ws_bytes < (size_t)w.bytes) return DHSA_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(ws_dev);
+    a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev; a.lse = lse_dev;
+    a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev;
+    a.n_part = reinterpret_cast<int *>(ws);
+    a.info = reinterpret_cast<int4 *>(ws + w.off_info);
+    a.state = reinterpret_cast<float2 *>(ws + w.off_state);
+    a.part = reinterpret_cast<float *>(ws + w.off_part);
+    if (weights_dev) a.norm = reinterpret_cast<float2 *>(ws + w.off_norm);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = a.T > 0 ? launch_span(a, prob->D, prob->dtype, s) : hipSuccess;
+    if (e == hipSuccess && weights_dev) e = launch_weights(a, prob->D, prob->dtype, weights_dev, decay, s);
+    return hip_status(e);
+}
+
+DHSA_API size_t dhsa_paged_evict_workspace_bytes(const dhsa_paged *prob, int32_t keep) {
+    SpanArgs a;
+    if (resolve_paged(prob, &a, nullptr) != DHSA_OK || keep < 1) return 0;
+    const int64_t lists = (int64_t)std::max(a.n_seq, 1) * a.H_kv;
+    return (size_t)(up256(lists * 4) + up256(lists * std::min<int64_t>(keep, a.slots_max) * 4));
+}
+
+DHSA_API dhsa_status dhsa_paged_evict(const dhsa_paged *prob, void *K_dev, void *V_dev, float *weights_dev,
+                                      const int32_t *table_dev, const int32_t *kv_len_dev, int32_t keep, int32_t first,
+                                      int32_t recent, const int32_t *table_out_dev, int32_t *kv_len_out_dev,
+                                      int32_t *idx_dev, void *ws_dev, size_t ws_bytes, void *stream) {
+    SpanArgs a;
+    const dhsa_status st = resolve_paged(prob, &a, nullptr);
+    if (st != DHSA_OK) return st;
+    if (keep < 1 || first < 0 || recent < 0 || (int64_t)first + recent > keep) return DHSA_ERR_BUDGET;
+    if (a.n_seq == 0) return DHSA_OK;
+    if (!K_dev || !V_dev || !weights_dev || !table_dev || !kv_len_dev || !table_out_dev || !kv_len_out_dev || !ws_dev)
+        return DHSA_ERR_NULL;
+    if (misaligned(K_dev) || misaligned(V_dev) || misaligned(ws_dev)) return DHSA_ERR_ALIGN;
+    if (ws_bytes < dhsa_paged_evict_workspace_bytes(prob, keep)) return DHSA_ERR_WORKSPACE;
+    a.table = table_dev; a.kv_len = kv_len_dev;
+    EvictArgs e;
+    e.K = (char *)K_dev; e.V = (char *)V_dev; e.weights = weights_dev;
+    e.table_out = table_out_dev; e.kv_out = kv_len_out_dev; e.idx = idx_dev;
+    e.keep = keep; e.first = first; e.recent = recent;
+    e.stride = (int)std::min<int64_t>(keep, a.slots_max);
+    e.count = static_cast<int32_t *>(ws_dev);
+    e.list = reinterpret_cast<int32_t *>(static_cast<char *>(ws_dev) + up256((int64_t)a.n_seq * a.H_kv * 4));
+    return hip_status(launch_evict(a, e, prob->D * (prob->dtype == DHSA_F32 ? 4 : 2), static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

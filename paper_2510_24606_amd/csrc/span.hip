@@ -1,0 +1,396 @@
+// Attention without routing over a range of keys: windows and paged caches (dhsa_window_prefill, dhsa_paged_attend).
+//
+// Work unit (find_item): 16 RB rows of one kv-head and sequence -- the query heads of a group lie side by side, row R is
+// token R / G -- and a piece of the keys that they see.  Four waves; each takes every fourth block of BK keys and all
+// rows, with K and V from memory straight into the registers that the matrix unit reads, so there is no barrier in the
+// loop; the waves' softmax states are joined at the end through LDS.
+//
+// Lane l = 16 q + n.  S^T (keys x rows) = K Q^T: the lane has the scores of row n against 4 keys 4 q + {0..3} of each 16.
+// These are, after the exponential, the B operand of O^T (columns x rows) += V^T P^T when the contraction runs over the keys
+// in that order.
+//   bf16, BK = 32 (v_mfma_f32_16x16x32_bf16): the lane loads 16 bytes (8 for D = 64) at column D/16 n of the keys
+//   {4 q + i, 16 + 4 q + i}, whole rows of V a quarter wave; operand j of V^T takes element j of each of the eight, put
+//   together by byte permutes.  Row m of output block j is column D/16 m + j.
+//   fp32, BK = 16 (v_mfma_f32_16x16x4_f32): K as 16 bytes at 16 s + 4 q, V as 16 bytes at 64 t + 4 n of key 4 q + i.  Row m
+//   of output block (t, j) is column 64 t + 4 m + j.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace dhsa {
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// Byte permutes: the low (high) halves of a and b, a below
+__device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
+__device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
+
+// What the two types differ in.  NC: columns of an output row that a lane has per output row m, all adjacent.
+template <typename T, int D, int RB> struct Tile;
+
+template <int D, int RB> struct Tile<bf16_t, D, RB> {
+    static constexpr int BK = 32, NT = D / 32, NJ = D / 16;
+    typedef uint32_t vload __attribute__((ext_vector_type(D == 128 ? 4 : 2)));
+    bf16x8_t qf[RB][NT];
+    f32x4_t o[RB][NJ];
+    struct Keys {
+        bf16x8_t k[2][NT];
+        vload v[8];
+    };
+    __device__ void load_q(int r, const char *row, int q) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) qf[r][t] = *reinterpret_cast<const bf16x8_t *>(row + 64 * t + 16 * q);
+    }
+    // offsets (16 bytes) of the block's rows are in LDS
+    __device__ static void load(Keys &x, const char *K, const char *V, const uint32_t *koff, const uint32_t *voff, int n, int q) {
+        uint32_t ko[2] = {koff[n], koff[16 + n]};
+        const uint4 v0 = *reinterpret_cast<const uint4 *>(voff + 4 * q), v1 = *reinterpret_cast<const uint4 *>(voff + 16 + 4 * q);
+        const uint32_t vo[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                x.k[h][t] = *reinterpret_cast<const bf16x8_t *>(K + ((uint64_t)ko[h] << 4) + 64 * t + 16 * q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x.v[i] = *reinterpret_cast<const vload *>(V + ((uint64_t)vo[i] << 4) + sizeof(vload) * n);
+    }
+    // keys that are not there: what was loaded in their place must not meet the matrix unit (0 times NaN)
+    __device__ static void clear(Keys &x, uint64_t bad, int q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (bad >> (16 * (i >> 2) + 4 * q + (i & 3)) & 1) x.v[i] = vload(0u);
+    }
+    // scores of row block r: s[8 keys], key 16 (x >> 2) + 4 q + (x & 3)
+    __device__ void scores(const Keys &x, int r, float *s) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.k[h][t], qf[r][t], acc, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[4 * h + i] = acc[i];
+        }
+    }
+    // probabilities are rounded to bf16, the type of the V that they meet in the matrix unit (as in dhsa_prefill)
+    __device__ void add(const Keys &x, const float (*p)[8]) {
+        bf16x8_t pf[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pf[r][i] = (__bf16)p[r][i];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            union { uint32_t w[4]; bf16x8_t v; } vt;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                vt.w[e] = (j & 1) ? halves_hi(x.v[2 * e][j >> 1], x.v[2 * e + 1][j >> 1])
+                                  : halves_lo(x.v[2 * e][j >> 1], x.v[2 * e + 1][j >> 1]);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt.v, pf[r], o[r][j], 0, 0, 0);
+        }
+    }
+    // column of element (j, i) of this lane's output row
+    __device__ static int column(int q, int j, int i) { return (4 * q + i) * NJ + j; }
+};
+
+template <int D, int RB> struct Tile<float, D, RB> {
+    static constexpr int BK = 16, NS = D / 16, NJ = D / 16;     // NJ = 4 (D / 64): output blocks (t, j)
+    f32x4_t qf[RB][NS];
+    f32x4_t o[RB][NJ];
+    struct Keys {
+        f32x4_t k[NS], v[4][D / 64];
+    };
+    __device__ void load_q(int r, const char *row, int q) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) qf[r][s] = *reinterpret_cast<const f32x4_t *>(row + 64 * s + 16 * q);
+    }
+    __device__ static void load(Keys &x, const char *K, const char *V, const uint32_t *koff, const uint32_t *voff, int n, int q) {
+        const uint32_t ko = koff[n];
+        const uint4 v0 = *reinterpret_cast<const uint4 *>(voff + 4 * q);
+        const uint32_t vo[4] = {v0.x, v0.y, v0.z, v0.w};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) x.k[s] = *reinterpret_cast<const f32x4_t *>(K + ((uint64_t)ko << 4) + 64 * s + 16 * q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < D / 64; ++t)
+                x.v[i][t] = *reinterpret_cast<const f32x4_t *>(V + ((uint64_t)vo[i] << 4) + 256 * t + 16 * n);
+    }
+    __device__ static void clear(Keys &x, uint64_t bad, int q) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (bad >> (4 * q + i) & 1)
+#pragma unroll
+                for (int t = 0; t < D / 64; ++t) x.v[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ void scores(const Keys &x, int r, float *s) const {
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[t][e], qf[r][t][e], acc, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = acc[i];
+    }
+    __device__ void add(const Keys &x, const float (*p)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+                    o[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[i][j >> 2][j & 3], p[r][i], o[r][j], 0, 0, 0);
+    }
+    __device__ static int column(int q, int j, int i) { return 64 * (j >> 2) + 4 * (4 * q + i) + (j & 3); }
+};
+
+__device__ __forceinline__ void store_out(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store_out(bf16_t *p, float x) {
+    union { __bf16 b; uint16_t u; } c;
+    c.b = (__bf16)x;
+    p->bits = c.u;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// grid: find_item's shares, from block0 on
+// ---------------------------------------------------------------------------
+template <typename T, int D, int RB, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
+    using Tl = Tile<T, D, RB>;
+    constexpr int M = 16 * RB, BK = Tl::BK, NP = BK / 4, NJ = Tl::NJ;
+    constexpr int kPad = D + 4;
+    struct Lists { alignas(16) uint32_t k[4][BK], v[4][BK]; };
+    struct Merge { float o[4][M][kPad]; float m[4][M], l[4][M]; };
+    __shared__ union { Lists li; Merge me; } sm;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, q = lane >> 4;
+    Item it;
+    if (!find_item(a, block0 + blockIdx.x, M, 4 * BK, &it)) return;
+    if (it.pieces > 1 && it.slot >= a.part_cap) return;      // (there are never so many)
+    const int base = it.q.kv - it.q.n;                       // position of the first new token
+    const int p_lo = base + it.R0 / a.G, p_hi = base + (it.R0 + it.rows - 1) / a.G;
+    const Span span = make_span(a, p_lo, p_hi);
+    const int units = (span.total + 4 * BK - 1) / (4 * BK), per = (units + it.pieces - 1) / it.pieces;
+    const int x_lo = it.piece * per * 4 * BK;
+    const int x_hi = x_lo + per * 4 * BK < span.total ? x_lo + per * 4 * BK : span.total;
+    const char *Kg = (const char *)a.K + it.g * a.ks_h, *Vg = (const char *)a.V + it.g * a.vs_h;
+    const int32_t *table = PAGED ? a.table + (int64_t)it.s * a.max_pages : nullptr;
+
+    Tl tl;
+    int pos[RB];
+    float m_ref[RB], l_run[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int row = 16 * r + n < it.rows ? 16 * r + n : it.rows - 1;    // rows past the end repeat the last one (never stored)
+        const int R = it.R0 + row, t = R / a.G, h = it.g * a.G + R % a.G;
+        tl.load_q(r, (const char *)((const T *)a.Q + h * a.qs_h + (it.q.q0 + t) * a.qs_t), q);
+        pos[r] = base + t;
+        m_ref[r] = -INFINITY;
+        l_run[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) tl.o[r][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    uint32_t *const koff = sm.li.k[wave], *const voff = sm.li.v[wave];
+    const float c = a.scale_log2e;
+    for (int x = x_lo + wave * BK; x < x_hi; x += 4 * BK) {
+        // places of the block's rows; keys past the end repeat the last one
+        const int xk = x + (lane & (BK - 1));
+        const int slot = span.slot(xk < x_hi ? xk : x_hi - 1);
+        bool bad = xk >= x_hi;
+        uint32_t ko, vo;
+        if constexpr (PAGED) {
+            const int pi = page_of(a, slot), in = slot - pi * a.page_size;
+            int page = table[pi];
+            if ((unsigned)page >= (unsigned)a.n_pages) { bad = true; page = 0; }
+            ko = (uint32_t)page * a.ks_p + (uint32_t)in * a.ks_s;
+            vo = (uint32_t)page * a.vs_p + (uint32_t)in * a.vs_s;
+        } else {
+            ko = (uint32_t)slot * a.ks_s;
+            vo = (uint32_t)slot * a.vs_s;
+        }
+        if (lane < BK) { koff[lane] = ko; voff[lane] = vo; }
+        // (a wave's LDS operations are executed in order: only the compiler has to keep them so)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        // does some row of the tile not see some key of the block?
+        const int hi_k = key_hi(a, slot);
+        const unsigned long long bad_m = __ballot(bad);
+        const bool masked = __any(bad || slot > p_lo || hi_k <= p_hi);
+        typename Tl::Keys kv;
+        Tl::load(kv, Kg, Vg, koff, voff, n, q);
+        if (PAGED && bad_m) Tl::clear(kv, bad_m, q);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        float p[RB][NP];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            float s[NP];
+            tl.scores(kv, r, s);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const int key = 16 * (i >> 2) + 4 * q + (i & 3), j = span.slot(x + key);
+                    const bool sees = j <= pos[r] && pos[r] < key_hi(a, j) && !(bad_m >> key & 1);
+                    s[i] = sees ? s[i] : -INFINITY;
+                }
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < NP; ++i) mx = fmaxf(mx, s[i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            // the reference is kept scaled and rounded: one that stays makes a factor of exactly 1
+            const float m_new = fmaxf(m_ref[r], mx * c);
+            const float ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m_ref[r] - ref);
+            m_ref[r] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                p[r][i] = __builtin_amdgcn_exp2f(s[i] * c - ref);
+                sum += p[r][i];
+            }
+            l_run[r] = l_run[r] * alpha + sum;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tl.o[r][j][i] *= alpha;
+        }
+        tl.add(kv, p);
+    }
+
+    // ---- join the four waves ----
+    __syncthreads();                          // the lists are dead
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        float l = l_run[r] + __shfl_xor(l_run[r], 16);
+        l += __shfl_xor(l, 32);
+        if (q == 0) {
+            sm.me.m[wave][16 * r + n] = m_ref[r];
+            sm.me.l[wave][16 * r + n] = l;
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sm.me.o[wave][16 * r + n][Tl::column(q, j, i)] = tl.o[r][j][i];
+    }
+    __syncthreads();
+    constexpr int LPR = 16;                   // lanes per row, D / 16 adjacent columns each
+    constexpr int CPL = D / LPR;
+    if (it.pieces > 1 && tid == 0) a.info[it.slot] = make_int4(it.piece == 0 ? it.pieces : 0, (int)it.q.q0, it.R0, it.rows);
+    for (int row = tid / LPR; row < it.rows; row += 256 / LPR) {
+        const int c0 = (tid % LPR) * CPL;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm.me.m[w][row]);
+        float l = 0.f, o[CPL];
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = sm.me.m[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm.me.m[w][row] - mx);
+            l += sm.me.l[w][row] * f;
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) o[e] += sm.me.o[w][row][c0 + e] * f;
+        }
+        if (it.pieces > 1) {
+            float *po = a.part + ((int64_t)it.slot * M + row) * D + c0;
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) po[e] = o[e];
+            if (c0 == 0) a.state[(int64_t)it.slot * M + row] = make_float2(mx, l);
+            continue;
+        }
+        const int R = it.R0 + row, h = it.g * a.G + R % a.G;
+        const int64_t t = it.q.q0 + R / a.G;
+        const float inv = l > 0.f ? 1.f / l : 0.f;         // no visible key: zeros
+        T *op = (T *)a.O + h * a.os_h + t * a.os_t + c0;
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) store_out(op + e, o[e] * inv);
+        if (c0 == 0) {
+            if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            if (a.norm) a.norm[h * a.T + t] = make_float2(mx, inv);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The pieces of cut tiles put together, a wave per row.  grid (part_cap, M / 4)
+// ---------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int M) {
+    const int slot = blockIdx.x, lane = threadIdx.x & 63;
+    if (slot >= *a.n_part) return;
+    const int4 in = a.info[slot];
+    const int row = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + (threadIdx.x >> 6));
+    if (in.x == 0 || row >= in.w) return;
+    constexpr int CPL = D / 64;
+    float mx = -INFINITY, l = 0.f, o[CPL];
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) o[e] = 0.f;
+    for (int x = 0; x < in.x; ++x) {
+        const int64_t at = ((int64_t)slot + (int64_t)x * a.H_kv) * M + row;
+        const float2 st = a.state[at];
+        if (st.x == -INFINITY) continue;
+        const float m_new = fmaxf(mx, st.x);
+        const float f0 = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new), f1 = __builtin_amdgcn_exp2f(st.x - m_new);
+        l = l * f0 + st.y * f1;
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) o[e] = o[e] * f0 + a.part[at * D + lane * CPL + e] * f1;
+        mx = m_new;
+    }
+    const int R = in.z + row, h = slot % a.H_kv * a.G + R % a.G;
+    const int64_t t = (int64_t)in.y + R / a.G;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T *op = (T *)a.O + h * a.os_h + t * a.os_t + lane * CPL;
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) store_out(op + e, o[e] * inv);
+    if (lane == 0) {
+        if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
+        if (a.norm) a.norm[h * a.T + t] = make_float2(mx, inv);
+    }
+}
+
+int span_rows(const SpanArgs &a, int) { return a.T * a.G > (int64_t)16 * std::max(a.n_seq, 1) ? 32 : 16; }
+
+int64_t span_target(const SpanArgs &, int) { return 1024; }
+
+hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
+    const int M = span_rows(a, dtype);
+    const int64_t tiles = a.T * a.G / M + std::min<int64_t>(a.n_seq, a.T);
+    const int64_t blocks = (tiles + (a.target + a.H_kv - 1) / a.H_kv) * a.H_kv;
+    for (int64_t b0 = 0; b0 < blocks; b0 += kGridMax) {
+        const dim3 grid((unsigned)std::min<int64_t>(blocks - b0, kGridMax));
+#define DHSA_SPAN2(T_, D_, RB) \
+    do { \
+        if (a.table) hipLaunchKernelGGL((k_span<T_, D_, RB, true>), grid, dim3(256), 0, s, a, (unsigned)b0); \
+        else hipLaunchKernelGGL((k_span<T_, D_, RB, false>), grid, dim3(256), 0, s, a, (unsigned)b0); \
+    } while (0)
+#define DHSA_SPAN1(T_, D_) do { if (M == 16) DHSA_SPAN2(T_, D_, 1); else DHSA_SPAN2(T_, D_, 2); } while (0)
+        if (dtype == DHSA_F32) { if (D == 64) DHSA_SPAN1(float, 64); else DHSA_SPAN1(float, 128); }
+        else { if (D == 64) DHSA_SPAN1(bf16_t, 64); else DHSA_SPAN1(bf16_t, 128); }
+#undef DHSA_SPAN1
+#undef DHSA_SPAN2
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.target > 0) {
+        const dim3 grid(a.part_cap, M / 4);
+        if (dtype == DHSA_F32) {
+            if (D == 64) hipLaunchKernelGGL((k_span_join<float, 64>), grid, dim3(256), 0, s, a, M);
+            else hipLaunchKernelGGL((k_span_join<float, 128>), grid, dim3(256), 0, s, a, M);
+        } else {
+            if (D == 64) hipLaunchKernelGGL((k_span_join<bf16_t, 64>), grid, dim3(256), 0, s, a, M);
+            else hipLaunchKernelGGL((k_span_join<bf16_t, 128>), grid, dim3(256), 0, s, a, M);
+        }
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dhsa
