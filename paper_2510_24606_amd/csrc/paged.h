@@ -25,7 +25,7 @@ struct SpanArgs {
     int64_t ks_h, vs_h;                             // bytes
     // pieces of key ranges: about `target` of them over all (0: every row tile has its range in one piece); what is cut
     // leaves the states of its rows in `part` (piece, row: D floats) and `state` (reference, sum), described in `info`
-    int target, part_cap;
+    int M, target, part_cap;     // M: rows of a tile
     float *part;
     float2 *state;
     int4 *info;                  // [part_cap] of each piece: pieces of the tile (0: not its first one), first token, first row, rows
@@ -153,8 +153,9 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
 }
 
 // ---- launchers ----
-int span_rows(const SpanArgs &a, int dtype);                        // M: rows of a tile
-int64_t span_target(const SpanArgs &a, int dtype);
+constexpr int kTallRows = 128;                                      // rows of a tile of span_tall.hip
+void choose_tiles(SpanArgs *a, int dtype, bool paged);              // sets M, target and part_cap: workspace and launches go by them
+hipError_t launch_span_tall(const SpanArgs &a, int D, unsigned blocks, unsigned block0, hipStream_t s);
 hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s);
 hipError_t launch_weights(const SpanArgs &a, int D, int dtype, float *weights, float decay, hipStream_t s);
 

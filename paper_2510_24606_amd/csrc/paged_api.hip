@@ -90,9 +90,8 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
 // Workspace of dhsa_paged_attend in bytes.
 struct PagedWs { int64_t off_info, off_state, off_part, off_norm, bytes; };
 PagedWs paged_ws(SpanArgs *a, int D, int dtype) {
-    a->target = (int)span_target(*a, dtype);
-    const int64_t M = span_rows(*a, dtype);
-    a->part_cap = a->target > 0 ? 2 * a->target + a->H_kv : 0;
+    choose_tiles(a, dtype, true);
+    const int64_t M = a->M;
     PagedWs w;
     w.off_info = 256;
     w.off_state = w.off_info + up256((int64_t)a->part_cap * 16);
@@ -133,6 +132,7 @@ DHSA_API dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t windo
     a.sinks = (int)std::min<int64_t>(sinks, INT_MAX);
     a.ks_s = L > 1 ? (uint32_t)(ks_l * esz / 16) : 0; a.vs_s = L > 1 ? (uint32_t)(vs_l * esz / 16) : 0;
     a.ks_h = ks_h * esz; a.vs_h = vs_h * esz;
+    choose_tiles(&a, prob->dtype, false);
     return hip_status(launch_span(a, prob->D, prob->dtype, static_cast<hipStream_t>(stream)));
 }
 

@@ -357,12 +357,16 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int M) {
     }
 }
 
-int span_rows(const SpanArgs &a, int) { return a.T * a.G > (int64_t)16 * std::max(a.n_seq, 1) ? 32 : 16; }
-
-int64_t span_target(const SpanArgs &, int) { return 1024; }
+void choose_tiles(SpanArgs *a, int dtype, bool paged) {
+    const int64_t rows = a->T * a->G, mean = rows / std::max(a->n_seq, 1);
+    a->M = mean > 16 ? 32 : 16;
+    if (dtype == DHSA_BF16 && mean > 48 && (paged || rows * a->H_kv >= 256 * kTallRows)) a->M = kTallRows;
+    a->target = !paged ? 0 : a->M == kTallRows ? 512 : 1024;
+    a->part_cap = paged ? 2 * a->target + a->H_kv : 0;
+}
 
 hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
-    const int M = span_rows(a, dtype);
+    const int M = a.M;
     const int64_t tiles = a.T * a.G / M + std::min<int64_t>(a.n_seq, a.T);
     const int64_t blocks = (tiles + (a.target + a.H_kv - 1) / a.H_kv) * a.H_kv;
     for (int64_t b0 = 0; b0 < blocks; b0 += kGridMax) {
@@ -373,6 +377,11 @@ hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
         else hipLaunchKernelGGL((k_span<T_, D_, RB, false>), grid, dim3(256), 0, s, a, (unsigned)b0); \
     } while (0)
 #define DHSA_SPAN1(T_, D_) do { if (M == 16) DHSA_SPAN2(T_, D_, 1); else DHSA_SPAN2(T_, D_, 2); } while (0)
+        if (M == kTallRows) {
+            const hipError_t e = launch_span_tall(a, D, grid.x, (unsigned)b0, s);
+            if (e != hipSuccess) return e;
+            continue;
+        }
         if (dtype == DHSA_F32) { if (D == 64) DHSA_SPAN1(float, 64); else DHSA_SPAN1(float, 128); }
         else { if (D == 64) DHSA_SPAN1(bf16_t, 64); else DHSA_SPAN1(bf16_t, 128); }
 #undef DHSA_SPAN1
