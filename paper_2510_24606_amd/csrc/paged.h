@@ -24,12 +24,12 @@ struct SpanArgs {
     uint32_t ks_p, ks_s, vs_p, vs_s;                // 16 bytes
     int64_t ks_h, vs_h;                             // bytes
     // pieces of key ranges: about `target` of them over all (0: every row tile has its range in one piece); what is cut
-    // leaves the states of its rows in `part` (piece, row: D floats) and `state` (reference, sum), described in `info`
+    // leaves the states of its rows in `part` (piece, row: D floats) and `state` (reference, sum), and in `cut` ([H_q][T]) where
+    // a row's first state is and how many pieces it has (one: the row is done)
     int M, target, part_cap;     // M: rows of a tile
     float *part;
     float2 *state;
-    int4 *info;                  // [part_cap] of each piece: pieces of the tile (0: not its first one), first token, first row, rows
-    int *n_part;                 // pieces of cut tiles
+    int2 *cut;
 };
 
 constexpr int kIntMaxP = 0x7fffffff;
@@ -91,8 +91,7 @@ struct Item {
 
 // Which share workgroup b has, M rows a tile and U keys a unit.  Every wave finds out for itself, without a barrier: lane i
 // looks at sequence 64 r + i.  A sequence's tiles all have as many pieces as its longest one needs, so that a piece has at most
-// P units, where P makes about `target` pieces of all.  Workgroup 0 also leaves the number of pieces of cut tiles for the
-// launch that joins them.  Later rows (longer ranges) come first.
+// P units, where P makes about `target` pieces of all.  Later rows (longer ranges) come first.
 __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, int U, Item *it) {
     const int lane = threadIdx.x & 63;
     const int g = (int)(b % (unsigned)a.H_kv), want = (int)(b / (unsigned)a.H_kv);
@@ -127,7 +126,7 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         const int np = tiles * pieces, cut = pieces > 1 ? np : 0;
         const int end = wave_incl_scan(np), cut_end = wave_incl_scan(cut);
         const int total = __builtin_amdgcn_readlane(end, 63), cut_total = __builtin_amdgcn_readlane(cut_end, 63);
-        if (!found && want < base + total) {
+        if (want < base + total) {
             const int from = base + end - np;
             const unsigned long long hit = __ballot(want >= from && want < base + end);
             const int l = __builtin_ctzll(hit);
@@ -146,9 +145,8 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         }
         base += total;
         part += cut_total;
-        if (found && b != 0) break;
+        if (found) break;
     }
-    if (b == 0 && threadIdx.x == 0 && a.target > 0) *a.n_part = part * a.H_kv < a.part_cap ? part * a.H_kv : a.part_cap;
     return found;
 }
 

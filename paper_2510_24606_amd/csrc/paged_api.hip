@@ -88,16 +88,17 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
 }
 
 // Workspace of dhsa_paged_attend in bytes.
-struct PagedWs { int64_t off_info, off_state, off_part, off_norm, bytes; };
+struct PagedWs { int64_t off_state, off_part, off_cut, off_norm, bytes; };
 PagedWs paged_ws(SpanArgs *a, int D, int dtype) {
     choose_tiles(a, dtype, true);
     const int64_t M = a->M;
     PagedWs w;
-    w.off_info = 256;
-    w.off_state = w.off_info + up256((int64_t)a->part_cap * 16);
+    const int64_t rows = a->T * a->H_kv * a->G;
+    w.off_state = 0;
     w.off_part = w.off_state + up256((int64_t)a->part_cap * M * 8);
-    w.off_norm = w.off_part + up256((int64_t)a->part_cap * M * D * 4);
-    w.bytes = w.off_norm + up256(a->T * a->H_kv * a->G * 8);
+    w.off_cut = w.off_part + up256((int64_t)a->part_cap * M * D * 4);
+    w.off_norm = w.off_cut + up256(rows * 8);
+    w.bytes = w.off_norm + up256(rows * 8);
     return w;
 }
 
@@ -175,8 +176,7 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
     char *ws = static_cast<char *>(ws_dev);
     a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev; a.lse = lse_dev;
     a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev;
-    a.n_part = reinterpret_cast<int *>(ws);
-    a.info = reinterpret_cast<int4 *>(ws + w.off_info);
+    a.cut = reinterpret_cast<int2 *>(ws + w.off_cut);
     a.state = reinterpret_cast<float2 *>(ws + w.off_state);
     a.part = reinterpret_cast<float *>(ws + w.off_part);
     if (weights_dev) a.norm = reinterpret_cast<float2 *>(ws + w.off_norm);

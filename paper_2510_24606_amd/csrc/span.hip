@@ -284,7 +284,6 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
     __syncthreads();
     constexpr int LPR = 16;                   // lanes per row, D / 16 adjacent columns each
     constexpr int CPL = D / LPR;
-    if (it.pieces > 1 && tid == 0) a.info[it.slot] = make_int4(it.piece == 0 ? it.pieces : 0, (int)it.q.q0, it.R0, it.rows);
     for (int row = tid / LPR; row < it.rows; row += 256 / LPR) {
         const int c0 = (tid % LPR) * CPL;
         float mx = -INFINITY;
@@ -300,6 +299,9 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 #pragma unroll
             for (int e = 0; e < CPL; ++e) o[e] += sm.me.o[w][row][c0 + e] * f;
         }
+        const int R = it.R0 + row, h = it.g * a.G + R % a.G;
+        const int64_t t = it.q.q0 + R / a.G;
+        if (c0 == 0 && it.piece == 0 && a.target > 0) a.cut[h * a.T + t] = make_int2(it.slot * M + row, it.pieces);
         if (it.pieces > 1) {
             float *po = a.part + ((int64_t)it.slot * M + row) * D + c0;
 #pragma unroll
@@ -307,8 +309,6 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
             if (c0 == 0) a.state[(int64_t)it.slot * M + row] = make_float2(mx, l);
             continue;
         }
-        const int R = it.R0 + row, h = it.g * a.G + R % a.G;
-        const int64_t t = it.q.q0 + R / a.G;
         const float inv = l > 0.f ? 1.f / l : 0.f;         // no visible key: zeros
         T *op = (T *)a.O + h * a.os_h + t * a.os_t + c0;
 #pragma unroll
@@ -321,39 +321,76 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 }
 
 // ---------------------------------------------------------------------------
-// The pieces of cut tiles put together, a wave per row.  grid (part_cap, M / 4)
+// The pieces of cut rows put together.  A workgroup looks at `per` rows at once and does the cut ones one after another: sixteen
+// lanes a piece, sixteen pieces side by side and four of each in flight.
 // ---------------------------------------------------------------------------
+constexpr int kJoinRows = 4096;     // workgroups, as long as each has at most 64 rows
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int M) {
-    const int slot = blockIdx.x, lane = threadIdx.x & 63;
-    if (slot >= *a.n_part) return;
-    const int4 in = a.info[slot];
-    const int row = __builtin_amdgcn_readfirstlane(blockIdx.y * 4 + (threadIdx.x >> 6));
-    if (in.x == 0 || row >= in.w) return;
-    constexpr int CPL = D / 64;
-    float mx = -INFINITY, l = 0.f, o[CPL];
+__global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
+    constexpr int CPL = D / 16, U = 4;
+    __shared__ float s_m[16], s_l[16], s_o[16][D];
+    const int tid = threadIdx.x, lane = tid & 63, grp = tid >> 4, c0 = (tid & 15) * CPL;
+    const int64_t rows = a.T * a.H_kv * a.G, r0 = (int64_t)blockIdx.x * per;
+    const int end = a.q_start[a.n_seq];          // rows from there on are nobody's: what lies in `cut` means nothing
+    int2 cut = make_int2(0, 0);
+    if (lane < per && r0 + lane < rows && (int)((r0 + lane) % a.T) < end) cut = a.cut[r0 + lane];
+    // (nor where the arrays are no sequences: nothing is read outside the states)
+    const bool is_cut = cut.y > 1 && cut.x >= 0 && cut.x / a.M + (int64_t)(cut.y - 1) * a.H_kv < a.part_cap;
+    for (unsigned long long left = __ballot(is_cut); left; left &= left - 1) {
+        const int i = __builtin_ctzll(left);
+        const int64_t at = __builtin_amdgcn_readlane(cut.x, i), step = (int64_t)a.H_kv * a.M;
+        const int pieces = __builtin_amdgcn_readlane(cut.y, i);
+        float mx = -INFINITY, l = 0.f, o[CPL];
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) o[e] = 0.f;
-    for (int x = 0; x < in.x; ++x) {
-        const int64_t at = ((int64_t)slot + (int64_t)x * a.H_kv) * M + row;
-        const float2 st = a.state[at];
-        if (st.x == -INFINITY) continue;
-        const float m_new = fmaxf(mx, st.x);
-        const float f0 = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - m_new), f1 = __builtin_amdgcn_exp2f(st.x - m_new);
-        l = l * f0 + st.y * f1;
+        for (int e = 0; e < CPL; ++e) o[e] = 0.f;
+        for (int x0 = grp; x0 < pieces; x0 += 16 * U) {
+            float2 st[U];
+            float po[U][CPL];
 #pragma unroll
-        for (int e = 0; e < CPL; ++e) o[e] = o[e] * f0 + a.part[at * D + lane * CPL + e] * f1;
-        mx = m_new;
-    }
-    const int R = in.z + row, h = slot % a.H_kv * a.G + R % a.G;
-    const int64_t t = (int64_t)in.y + R / a.G;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T *op = (T *)a.O + h * a.os_h + t * a.os_t + lane * CPL;
+            for (int u = 0; u < U; ++u) {
+                const int64_t x = at + step * (x0 + 16 * u < pieces ? x0 + 16 * u : x0);
+                st[u] = a.state[x];
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) store_out(op + e, o[e] * inv);
-    if (lane == 0) {
-        if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
-        if (a.norm) a.norm[h * a.T + t] = make_float2(mx, inv);
+                for (int e = 0; e < CPL; ++e) po[u][e] = a.part[x * D + c0 + e];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (x0 + 16 * u >= pieces || st[u].x == -INFINITY) continue;
+                const float m_new = fmaxf(mx, st[u].x);
+                const float f0 = __builtin_amdgcn_exp2f(mx - m_new), f1 = __builtin_amdgcn_exp2f(st[u].x - m_new);
+                l = l * f0 + st[u].y * f1;
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) o[e] = o[e] * f0 + po[u][e] * f1;
+                mx = m_new;
+            }
+        }
+        __syncthreads();                         // the row before has been read
+        if (c0 == 0) { s_m[grp] = mx; s_l[grp] = l; }
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) s_o[grp][c0 + e] = o[e];
+        __syncthreads();
+        if (tid < D) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) m = fmaxf(m, s_m[x]);
+            float sum = 0.f, acc = 0.f;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const float f = s_m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[x] - m);
+                sum += s_l[x] * f;
+                acc += s_o[x][tid] * f;
+            }
+            const int64_t r = r0 + i;
+            const int h = (int)(r / a.T);
+            const int64_t t = r - h * a.T;
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            store_out((T *)a.O + h * a.os_h + t * a.os_t + tid, acc * inv);
+            if (tid == 0) {
+                if (a.lse) a.lse[r] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+                if (a.norm) a.norm[r] = make_float2(m, inv);
+            }
+        }
     }
 }
 
@@ -390,14 +427,13 @@ hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (a.target > 0) {
-        const dim3 grid(a.part_cap, M / 4);
-        if (dtype == DHSA_F32) {
-            if (D == 64) hipLaunchKernelGGL((k_span_join<float, 64>), grid, dim3(256), 0, s, a, M);
-            else hipLaunchKernelGGL((k_span_join<float, 128>), grid, dim3(256), 0, s, a, M);
-        } else {
-            if (D == 64) hipLaunchKernelGGL((k_span_join<bf16_t, 64>), grid, dim3(256), 0, s, a, M);
-            else hipLaunchKernelGGL((k_span_join<bf16_t, 128>), grid, dim3(256), 0, s, a, M);
-        }
+        const int64_t rows = a.T * a.H_kv * a.G;
+        const int per = (int)std::min<int64_t>(64, (rows + kJoinRows - 1) / kJoinRows);
+        const dim3 grid((unsigned)((rows + per - 1) / per));
+#define DHSA_JOIN(T_, D_) hipLaunchKernelGGL((k_span_join<T_, D_>), grid, dim3(256), 0, s, a, per)
+        if (dtype == DHSA_F32) { if (D == 64) DHSA_JOIN(float, 64); else DHSA_JOIN(float, 128); }
+        else { if (D == 64) DHSA_JOIN(bf16_t, 64); else DHSA_JOIN(bf16_t, 128); }
+#undef DHSA_JOIN
     }
     return hipGetLastError();
 }

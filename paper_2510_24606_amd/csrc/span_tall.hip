@@ -297,10 +297,11 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
 #undef TALL_PV
 
     // lane: row lr of the block, columns 32 db + 8 q4 + 4 g2 + {0..3}
-    if (it.pieces > 1 && tid == 0) a.info[it.slot] = make_int4(it.piece == 0 ? it.pieces : 0, (int)it.q.q0, it.R0, it.rows);
     if (!live) return;
     const float l = l_run + __shfl_xor(l_run, 32), mx = m_ref != m_ref ? -INFINITY : m_ref * c;
     if (pad_row) return;
+    const int64_t t = it.q.q0 + tok;
+    if (g2 == 0 && it.piece == 0 && a.target > 0) a.cut[h * a.T + t] = make_int2(it.slot * kTallRows + rb * 32 + lr, it.pieces);
     if (it.pieces > 1) {
         const int64_t at = (int64_t)it.slot * kTallRows + rb * 32 + lr;
         float *po = a.part + at * D;
@@ -313,7 +314,6 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
         if (g2 == 0) a.state[at] = make_float2(mx, l);
         return;
     }
-    const int64_t t = it.q.q0 + tok;
     const float inv = l > 0.f ? 1.f / l : 0.f;   // no visible key: zeros
     uint16_t *op = (uint16_t *)a.O + h * a.os_h + t * a.os_t;
 #pragma unroll
