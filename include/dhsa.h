@@ -417,14 +417,15 @@ dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, con
  *   weights = decay weights + sum over the call's rows and the query heads of the kv-head of
  *             exp(q . k scale - lse)
  * (decay in [0, 1]; with 0 the old values are not read; else DHSA_ERR_SHAPE).  The sums are made in a fixed order.
- * ws_dev: scratch of dhsa_paged_workspace_bytes(prob) bytes, 16-byte aligned, nothing in which
- * has to be set; calls that share it must be ordered.  The size depends on T, n_seq and the
- * head counts only. */
+ * ws_dev: scratch of dhsa_paged_workspace_bytes(prob, weights) bytes (weights: 0 where weights_dev
+ * is NULL), 16-byte aligned, nothing in which has to be set; calls that share it must be ordered.  The
+ * size depends on T, n_seq, the head counts and D; with weights and few new tokens a sequence also on the
+ * pool (4 bytes for each slot and query head and token of a sequence: scores that are not computed twice). */
 dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev, const void *K_dev, const void *V_dev,
                               const int32_t *table_dev, const int32_t *q_start_dev, const int32_t *kv_len_dev,
                               void *O_dev, float *lse_dev, float *weights_dev, float decay, void *ws_dev,
                               size_t ws_bytes, void *stream);
-size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob);   /* 0 on invalid arguments */
+size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob, int weights);   /* 0 on invalid arguments */
 
 /* Every sequence of more than `keep` tokens is cut down to `keep`: of each kv-head the slots
  * [0, first) and the last `recent` stay, and of the others those with the largest weights (equal

@@ -123,7 +123,7 @@ def lib() -> C.CDLL:
         l.dhsa_paged_append.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp]; l.dhsa_paged_append.restype = C.c_int
         l.dhsa_paged_attend.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
         l.dhsa_paged_attend.restype = C.c_int
-        l.dhsa_paged_workspace_bytes.argtypes = [G]; l.dhsa_paged_workspace_bytes.restype = C.c_size_t
+        l.dhsa_paged_workspace_bytes.argtypes = [G, C.c_int]; l.dhsa_paged_workspace_bytes.restype = C.c_size_t
         l.dhsa_paged_evict.argtypes = [G, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_size_t, vp]
         l.dhsa_paged_evict.restype = C.c_int
         l.dhsa_paged_evict_workspace_bytes.argtypes = [G, C.c_int32]; l.dhsa_paged_evict_workspace_bytes.restype = C.c_size_t
@@ -397,17 +397,17 @@ def paged_problem(K, V, table, H_q: int, T: int, window: int = 0, sinks: int = 0
     return p
 
 
-def dhsa_paged_workspace_bytes(prob: dhsa_paged) -> int:
-    return int(lib().dhsa_paged_workspace_bytes(C.byref(prob)))
+def dhsa_paged_workspace_bytes(prob: dhsa_paged, weights: bool = True) -> int:
+    return int(lib().dhsa_paged_workspace_bytes(C.byref(prob), int(weights)))
 
 
 def dhsa_paged_evict_workspace_bytes(prob: dhsa_paged, keep: int) -> int:
     return int(lib().dhsa_paged_evict_workspace_bytes(C.byref(prob), keep))
 
 
-def alloc_paged(prob: dhsa_paged, device="cuda"):
-    """Workspace of dhsa_paged_attend: of a problem with as many new tokens and sequences, whatever their lengths."""
-    n = dhsa_paged_workspace_bytes(prob)
+def alloc_paged(prob: dhsa_paged, device="cuda", weights: bool = True):
+    """Workspace of dhsa_paged_attend (weights = False: of calls without weights), whatever the sequences' lengths."""
+    n = dhsa_paged_workspace_bytes(prob, weights)
     if n == 0:
         raise DhsaError(2, "problem rejected by dhsa_paged_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device)

@@ -30,9 +30,17 @@ struct SpanArgs {
     float *part;
     float2 *state;
     int2 *cut;
+    int g_shift;                 // R / G = R g_mul >> g_shift
+    uint32_t g_mul;
+    // scores of sequences of at most kFewRows rows a kv-head, for the weights (nullptr: none are kept): score_units blocks of 64;
+    // a row has ceil(kv / 64) blocks, its packed keys in order
+    float *scores;
+    int score_units;
 };
 
 constexpr int kIntMaxP = 0x7fffffff;
+constexpr int kFewRows = 32;
+constexpr int kScoreUnitsMax = 1 << 24;      // 4 GiB; 64 times that fits 32 bits
 
 // One sequence as the kernels see it: whatever is in the arrays, rows stay below T and slots below slots_max.
 struct Seq {
@@ -74,6 +82,20 @@ __device__ __forceinline__ int page_of(const SpanArgs &a, int slot) {
     return (int)(((uint64_t)(uint32_t)slot * a.div_mul) >> a.div_shift);
 }
 
+__device__ __forceinline__ int token_of(const SpanArgs &a, int R) {
+    return (int)(((uint64_t)(uint32_t)R * a.g_mul) >> a.g_shift);
+}
+
+// Blocks of kept scores that a sequence needs: 0 if none are kept of it.  Sequences get theirs one after another; one that
+// would end behind score_units has none (its weights are made from Q and K again).
+__device__ __forceinline__ int score_need(const SpanArgs &a, const Seq &q) {
+    const int64_t rows = (int64_t)q.n * a.G;
+    if (!a.scores || rows > kFewRows) return 0;
+    const int64_t need = rows * a.H_kv * ((q.kv + 63) >> 6);
+    return need > kScoreUnitsMax ? kScoreUnitsMax + 1 : (int)need;
+}
+__device__ __forceinline__ int capped(int units) { return units > kScoreUnitsMax ? kScoreUnitsMax + 1 : units; }   // (fits no workspace)
+
 // fp32 sum over the wave, in every lane; the order is fixed
 __device__ __forceinline__ float wave_sum(float x) {
 #define DHSA_STEP(CTRL, ROWS) x += __int_as_float(dpp_or<CTRL, ROWS>(0, __float_as_int(x)));
@@ -87,6 +109,8 @@ __device__ __forceinline__ float wave_sum(float x) {
 struct Item {
     Seq q;
     int s, g, R0, rows, piece, pieces, slot;
+    float *scores;   // of row R0, or nullptr
+    int score_row;   // from row to row
 };
 
 // Which share workgroup b has, M rows a tile and U keys a unit.  Every wave finds out for itself, without a barrier: lane i
@@ -118,7 +142,7 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         const float p = cost * (float)a.H_kv / (float)a.target;
         P = p < 1e9f ? (int)(p * 1.00001f) + 1 : 1000000000;
     }
-    int base = 0, part = 0;
+    int base = 0, part = 0, units_before = 0;
     bool found = false;
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
         if (s0 > 0 || a.n_seq > 64 || a.target <= 0) measure(s0 + lane, &q, &tiles, &units);
@@ -126,6 +150,11 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         const int np = tiles * pieces, cut = pieces > 1 ? np : 0;
         const int end = wave_incl_scan(np), cut_end = wave_incl_scan(cut);
         const int total = __builtin_amdgcn_readlane(end, 63), cut_total = __builtin_amdgcn_readlane(cut_end, 63);
+        int need = 0, need_end = 0;
+        if (a.scores) {
+            need = s0 + lane < a.n_seq ? score_need(a, q) : 0;
+            need_end = wave_incl_scan(need);
+        }
         if (want < base + total) {
             const int from = base + end - np;
             const unsigned long long hit = __ballot(want >= from && want < base + end);
@@ -141,8 +170,14 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
             const int64_t left = (int64_t)it->q.n * a.G - it->R0;
             it->rows = left < M ? (int)left : M;
             it->slot = it->pieces > 1 ? (part + of(cut_end - cut) + at) * a.H_kv + g : -1;
+            it->scores = nullptr;
+            it->score_row = (it->q.kv + 63) >> 6 << 6;
+            const int units = of(need), end_units = capped(units_before + of(need_end));
+            if (units > 0 && end_units <= a.score_units)
+                it->scores = a.scores + (int64_t)(end_units - units) * 64 + ((int64_t)g * it->q.n * a.G + it->R0) * it->score_row;
             found = true;
         }
+        units_before = capped(units_before + __builtin_amdgcn_readlane(need_end, 63));
         base += total;
         part += cut_total;
         if (found) break;

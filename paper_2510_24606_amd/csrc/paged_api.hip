@@ -16,13 +16,13 @@ namespace {
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
-// slot / page_size as a multiplication: with l = ceil(log2 d) and mul = floor(2^(31 + l) / d) + 1 < 2^32, mul d - 2^(31 + l) is
+// x / d as a multiplication: with l = ceil(log2 d) and mul = floor(2^(31 + l) / d) + 1 < 2^32, mul d - 2^(31 + l) is
 // in 1 .. d <= 2^l, so x mul / 2^(31 + l) is above x / d by less than 1 / d for x < 2^31
-void set_divisor(uint32_t d, SpanArgs *a) {
+void set_divisor(uint32_t d, uint32_t *mul, int *shift) {
     int l = 0;
     while (((uint64_t)1 << l) < d) ++l;
-    a->div_mul = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
-    a->div_shift = 31 + l;
+    *mul = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
+    *shift = 31 + l;
 }
 
 // What the two problem structs have in common.
@@ -34,6 +34,7 @@ dhsa_status heads(int64_t H_q, int64_t H_kv, int32_t D, int32_t dtype, float sca
     *a = SpanArgs{};
     a->H_kv = (int)H_kv;
     a->G = (int)(H_q / H_kv);
+    set_divisor((uint32_t)a->G, &a->g_mul, &a->g_shift);
     a->scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
     return DHSA_OK;
 }
@@ -76,7 +77,7 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
     a->n_seq = in->n_seq;
     a->n_pages = in->n_pages; a->max_pages = in->max_pages; a->page_size = in->page_size;
     a->slots_max = in->page_size * in->max_pages;
-    set_divisor((uint32_t)in->page_size, a);
+    set_divisor((uint32_t)in->page_size, &a->div_mul, &a->div_shift);
     a->window = in->window == 0 || in->window > INT_MAX ? INT_MAX : (int)in->window;
     a->sinks = (int)std::min<int64_t>(in->sinks, INT_MAX);
     // (a stride of a single page or slot is not used and may not fit)
@@ -88,8 +89,8 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
 }
 
 // Workspace of dhsa_paged_attend in bytes.
-struct PagedWs { int64_t off_state, off_part, off_cut, off_norm, bytes; };
-PagedWs paged_ws(SpanArgs *a, int D, int dtype) {
+struct PagedWs { int64_t off_state, off_part, off_cut, off_norm, off_scores, bytes; };
+PagedWs paged_ws(SpanArgs *a, int D, int dtype, bool weights) {
     choose_tiles(a, dtype, true);
     const int64_t M = a->M;
     PagedWs w;
@@ -98,7 +99,17 @@ PagedWs paged_ws(SpanArgs *a, int D, int dtype) {
     w.off_part = w.off_state + up256((int64_t)a->part_cap * M * 8);
     w.off_cut = w.off_part + up256((int64_t)a->part_cap * M * D * 4);
     w.off_norm = w.off_cut + up256(rows * 8);
-    w.bytes = w.off_norm + up256(rows * 8);
+    w.off_scores = w.off_norm + (weights ? up256(rows * 8) : 0);
+    // Scores that are kept for the weights: every slot of the pool once, for as many rows as a sequence has in the mean (a
+    // step of a batch has the same number of each).  What does not fit is computed again.
+    a->score_units = 0;
+    if (weights && a->M <= kFewRows && a->T > 0 && a->n_seq > 0) {
+        const int64_t mean = (a->T * a->G + a->n_seq - 1) / a->n_seq, pool = (int64_t)a->n_pages * a->page_size;
+        const int64_t every = a->T * a->G * ((a->slots_max + 63) / 64);      // of a kv-head, were all sequences as long as they can be
+        const int64_t once = std::min(mean, (int64_t)kFewRows) * (pool / 64) + a->T * a->G;
+        a->score_units = (int)std::min<int64_t>(std::min(every, once) * a->H_kv, kScoreUnitsMax);
+    }
+    w.bytes = w.off_scores + (int64_t)a->score_units * 256;
     return w;
 }
 
@@ -153,10 +164,10 @@ DHSA_API dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new
     return hip_status(launch_append(a, ap, prob->D * (prob->dtype == DHSA_F32 ? 4 : 2), static_cast<hipStream_t>(stream)));
 }
 
-DHSA_API size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob) {
+DHSA_API size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob, int weights) {
     SpanArgs a;
     if (resolve_paged(prob, &a, nullptr) != DHSA_OK) return 0;
-    return (size_t)paged_ws(&a, prob->D, prob->dtype).bytes;
+    return (size_t)std::max<int64_t>(paged_ws(&a, prob->D, prob->dtype, weights != 0).bytes, 256);
 }
 
 DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev, const void *K_dev, const void *V_dev,
@@ -171,7 +182,7 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
     if ((a.T > 0 && (!Q_dev || !O_dev)) || !K_dev || !V_dev || !table_dev || !q_start_dev || !kv_len_dev || !ws_dev)
         return DHSA_ERR_NULL;
     if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(ws_dev)) return DHSA_ERR_ALIGN;
-    const PagedWs w = paged_ws(&a, prob->D, prob->dtype);
+    const PagedWs w = paged_ws(&a, prob->D, prob->dtype, weights_dev != nullptr);
     if (ws_bytes < (size_t)w.bytes) return DHSA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(ws_dev);
     a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev; a.lse = lse_dev;
@@ -180,6 +191,7 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
     a.state = reinterpret_cast<float2 *>(ws + w.off_state);
     a.part = reinterpret_cast<float *>(ws + w.off_part);
     if (weights_dev) a.norm = reinterpret_cast<float2 *>(ws + w.off_norm);
+    if (a.score_units > 0) a.scores = reinterpret_cast<float *>(ws + w.off_scores);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = a.T > 0 ? launch_span(a, prob->D, prob->dtype, s) : hipSuccess;
     if (e == hipSuccess && weights_dev) e = launch_weights(a, prob->D, prob->dtype, weights_dev, decay, s);

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const int row = 16 * r + n < it.rows ? 16 * r + n : it.rows - 1;    // rows past the end repeat the last one (never stored)
-        const int R = it.R0 + row, t = R / a.G, h = it.g * a.G + R % a.G;
+        const int R = it.R0 + row, t = token_of(a, R), h = it.g * a.G + R - t * a.G;
         tl.load_q(r, (const char *)((const T *)a.Q + h * a.qs_h + (it.q.q0 + t) * a.qs_t), q);
         pos[r] = base + t;
         m_ref[r] = -INFINITY;
@@ -240,6 +240,13 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
                     const bool sees = j <= pos[r] && pos[r] < key_hi(a, j) && !(bad_m >> key & 1);
                     s[i] = sees ? s[i] : -INFINITY;
                 }
+            }
+            // (a block ends inside its row's share: the share is whole blocks of 64, pieces begin at multiples of 4 BK)
+            if (it.scores && 16 * r + n < it.rows) {
+                float *to = it.scores + (int64_t)(16 * r + n) * it.score_row + x + 4 * q;
+#pragma unroll
+                for (int h = 0; h < NP / 4; ++h)
+                    *reinterpret_cast<f32x4_t *>(to + 16 * h) = f32x4_t{s[4 * h] * c, s[4 * h + 1] * c, s[4 * h + 2] * c, s[4 * h + 3] * c};
             }
             float mx = s[0];
 #pragma unroll
@@ -315,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
         for (int e = 0; e < CPL; ++e) store_out(op + e, o[e] * inv);
         if (c0 == 0) {
             if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
-            if (a.norm) a.norm[h * a.T + t] = make_float2(mx, inv);
+            if (a.norm) a.norm[h * a.T + t] = make_float2(l > 0.f ? mx : 1e30f, inv);
         }
     }
 }
@@ -388,7 +395,7 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
             store_out((T *)a.O + h * a.os_h + t * a.os_t + tid, acc * inv);
             if (tid == 0) {
                 if (a.lse) a.lse[r] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
-                if (a.norm) a.norm[r] = make_float2(m, inv);
+                if (a.norm) a.norm[r] = make_float2(sum > 0.f ? m : 1e30f, inv);
             }
         }
     }

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
     // on the same SIMD); a row that is not there has q = 0 and a reference that makes every p 0
     const int rb = (wave + (blockIdx.x >> 3)) & 3;
     const bool live = rb * 32 < it.rows, pad_row = rb * 32 + lr >= it.rows;
-    const int R = it.R0 + (pad_row ? it.rows - 1 : rb * 32 + lr), tok = R / a.G, h = it.g * a.G + R % a.G;
+    const int R = it.R0 + (pad_row ? it.rows - 1 : rb * 32 + lr), tok = token_of(a, R), h = it.g * a.G + R - tok * a.G;
     const int pos = base + tok;
     bf16x8 qf[NS];
     {
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
         }
     if (g2 == 0) {
         if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
-        if (a.norm) a.norm[h * a.T + t] = make_float2(mx, inv);
+        if (a.norm) a.norm[h * a.T + t] = make_float2(l > 0.f ? mx : 1e30f, inv);
     }
 }
 

@@ -1,130 +1,296 @@
-// What each cached key has got of attention (dhsa_paged_attend with weights): the scores are made again from Q and K, and with
-// the exponent reference and the sum of each row, which attention has left, every probability is known at once.
+// What each cached key has got of attention (dhsa_paged_attend with weights).  With the exponent reference and the sum of each row,
+// which attention has left, a score gives its probability at once: exp2(s c - reference) / sum.  Every key's sum over rows and heads
+// is made by one workgroup in a fixed order; nothing is added with atomics.
 //
-// Work unit: 64 keys of a kv-head and sequence.  They stay in the registers that the matrix unit reads; the rows that see
-// them pass by, every fourth block of 16 to each of the four waves.  S^T (keys x rows) = K Q^T: a lane adds up the
-// probabilities of its 16 keys over its rows, the 16 lanes of other rows and the four waves follow once at the end, so the
-// order of a sum is fixed and nothing is added with atomics.
+// A workgroup takes shares of two kinds, one after another:
+//   * 1024 keys of a kv-head of a sequence whose scores were kept (few rows): they are read, four keys a thread.
+//   * otherwise the scores are made again from Q and K.  bf16: 128 keys, 32 in the registers of each wave, and the rows that see
+//     them staged through LDS in blocks of 64 (K from memory once, Q once per 128 keys).  S^T (keys x rows) = K Q^T, so a lane
+//     has 16 keys of one row: it adds up its own keys over its rows, and the 32 rows of a block follow once at the end.  Bound
+//     by the vector unit: an exponential, a product and two sums a pair beside 16 cycles of matrix unit for 64 pairs.
+//     fp32: 64 keys in the registers of every wave, each of which takes every fourth block of 16 rows.
 #include <algorithm>
 
+#include "attn_mfma.h"
 #include "paged.h"
 
 namespace dhsa {
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// 16 bytes of a row as the matrix unit takes them: element e of step t is column 32 t + 8 q + e (bf16) or 16 t + 4 q + e (fp32)
-template <typename T> struct Frag;
-template <> struct Frag<bf16_t> {
-    typedef bf16x8_t type;
-    __device__ static f32x4_t mfma(const type &k, const type &x, f32x4_t acc) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x, acc, 0, 0, 0);
-    }
+constexpr int kKeptKeys = 1024;
+
+template <typename T> struct Heavy;
+template <> struct Heavy<bf16_t> { static constexpr int kKeys = 128, kRows = 64; };
+template <> struct Heavy<float> { static constexpr int kKeys = 64, kRows = 16; };
+
+template <typename T, int D> struct WeightsSmem;
+template <int D> struct WeightsSmem<bf16_t, D> {
+    alignas(1024) uint16_t q[2][64 * D];
+    float2 norm[2][64];
+    int pos[2][64];
+    float sum[128];
 };
-template <> struct Frag<float> {
-    typedef f32x4_t type;
-    __device__ static f32x4_t mfma(const type &k, const type &x, f32x4_t acc) {
+template <int D> struct WeightsSmem<float, D> {
+    float sum[4][64];
+};
+
+// The rows (of a kv-head) that may see one of the keys j0 .. j1: [r0, r1)
+__device__ __forceinline__ void rows_of(const SpanArgs &a, const Seq &sq, int j0, int j1, int *r0, int *r1) {
+    const int base = sq.kv - sq.n;
+    const int t0 = j0 > base ? j0 - base : 0;
+    const int far = key_hi(a, j1);                     // no position from here on sees the last key
+    const int t1 = j0 < a.sinks || far >= sq.kv ? sq.n : far - base;
+    *r0 = t0 * a.G;
+    *r1 = t1 > t0 ? t1 * a.G : *r0;
+}
+
+__device__ __forceinline__ void put_weight(const SpanArgs &a, const int32_t *table, int g, int j, float *W, float decay, float x) {
+    const int pi = page_of(a, j), page = table[pi];
+    if ((unsigned)page >= (unsigned)a.n_pages) return;
+    float *w = W + ((int64_t)page * a.H_kv + g) * a.page_size + (j - pi * a.page_size);
+    *w = decay > 0.f ? decay * *w + x : x;
+}
+
+__device__ __forceinline__ void load16_to_lds(uint64_t addr, unsigned lds_window) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds_window) : "memory");
+#else
+    (void)addr; (void)lds_window;
+#endif
+}
+
+// byte address of row j of K of kv-head g (a page that is none: page 0, whose sums are not written)
+__device__ __forceinline__ const char *key_row(const SpanArgs &a, const int32_t *table, int g, int j) {
+    const int pi = page_of(a, j);
+    int page = table[pi];
+    if ((unsigned)page >= (unsigned)a.n_pages) page = 0;
+    return (const char *)a.K + g * a.ks_h + ((uint64_t)((uint32_t)page * a.ks_p + (uint32_t)(j - pi * a.page_size) * a.ks_s) << 4);
+}
+
+// ---- bf16: the sums of keys j0 .. j0 + keys - 1 (at most 128), left in sm.sum ----
+template <int D>
+__device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const SpanArgs &a, const Seq &sq, const int32_t *table, int g, int j0,
+                                           int keys) {
+    constexpr int OPR = D / 8, NS = D / 16, LPS = 64 * OPR / 256, RPW = 64 / OPR;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lr = lane & 31, g2 = lane >> 5, base = sq.kv - sq.n;
+    const float c = a.scale_log2e;
+    int R0, R1;
+    rows_of(a, sq, j0, j0 + keys - 1, &R0, &R1);
+    const int kw = j0 + 32 * wave;                     // this wave's first key
+    bf16x8 kf[NS];
+    {
+        const char *row = key_row(a, table, g, kw + lr < j0 + keys ? kw + lr : j0 + keys - 1) + 16 * g2;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], x[e], acc, 0, 0, 0);
-        return acc;
+        for (int s = 0; s < NS; ++s) kf[s] = *reinterpret_cast<const bf16x8 *>(row + 32 * s);
     }
-};
+    // staging: load i of a wave fills the KiB 4 i + wave of the stage; pieces of a row are swizzled as in span_tall.hip
+    const int ld_row0 = wave * RPW + lane / OPR;
+    const unsigned ld_piece = 16u * ((lane % OPR) ^ piece_swizzle(ld_row0, OPR));
+    const unsigned lds_q = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)sm.q;
+    const int q_sw = piece_swizzle(lr, OPR);
+    const uint16_t *Qg = (const uint16_t *)a.Q + (int64_t)g * a.G * a.qs_h + sq.q0 * a.qs_t;
+    const auto ask = [&](int R, int buf) {
+#pragma unroll
+        for (int i = 0; i < LPS; ++i) {
+            const int r = R + ld_row0 + 4 * RPW * i, rr = r < R1 ? r : R1 - 1, t = token_of(a, rr), h = rr - t * a.G;
+            load16_to_lds((uint64_t)(uintptr_t)(Qg + h * a.qs_h + t * a.qs_t) + ld_piece, lds_q + buf * 128 * D + wave * 1024 + 4096 * i);
+        }
+    };
+    float2 nm;
+    int nt;
+    const auto ask_norm = [&](int R) {                 // threads 0 .. 63; a row that is not there gets p = 0
+        const int r = R + lane, rr = r < R1 ? r : R1 - 1;
+        nt = token_of(a, rr);
+        nm = a.norm[(int64_t)(g * a.G + rr - nt * a.G) * a.T + sq.q0 + nt];
+        if (r >= R1) nm = make_float2(1e30f, 0.f);
+    };
+    const auto put_norm = [&](int buf) { sm.norm[buf][lane] = nm; sm.pos[buf][lane] = base + nt; };
+
+    f32x16 sum;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sum[x] = 0.f;
+    __syncthreads();                                   // the stages and sums of the share before have been read
+    if (R0 < R1) {
+        ask(R0, 0);
+        if (wave == 0) { ask_norm(R0); put_norm(0); }
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0)
+        __syncthreads();
+        const int k_last = kw + 31 < sq.kv ? kw + 31 : sq.kv - 1, k_far = kw < a.sinks && k_last < a.sinks ? kIntMaxP : key_hi(a, kw < a.sinks ? a.sinks : kw);
+        for (int R = R0, buf = 0; R < R1; R += 64, buf ^= 1) {
+            const bool more = R + 64 < R1;
+            if (more) {
+                ask(R + 64, buf ^ 1);
+                if (wave == 0) ask_norm(R + 64);
+            }
+            // do all rows of the stage see all keys of the wave?
+            const int p0 = base + token_of(a, R), p1 = base + token_of(a, R + 63 < R1 ? R + 63 : R1 - 1);
+            const bool masked = k_last > p0 || k_far <= p1;
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                f32x16 s_;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) s_[x] = 0.f;
+                const char *qp = (const char *)sm.q[buf] + 2 * (rb * 32 + lr) * D;
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+                    s_ = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], *reinterpret_cast<const bf16x8 *>(qp + 16 * ((2 * s + g2) ^ q_sw)), s_, 0, 0, 0);
+                const float2 row = sm.norm[buf][rb * 32 + lr];
+                if (masked) {
+                    const int p = sm.pos[buf][rb * 32 + lr];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const int j = kw + (x & 3) + 8 * (x >> 2) + 4 * g2;
+                        s_[x] = j <= p && p < key_hi(a, j) ? s_[x] : -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 16; ++x) sum[x] += __builtin_amdgcn_exp2f(s_[x] * c - row.x) * row.y;
+            }
+            if (more && wave == 0) put_norm(buf ^ 1);
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+        float v = sum[x];
+        v += __shfl_xor(v, 1); v += __shfl_xor(v, 2); v += __shfl_xor(v, 4); v += __shfl_xor(v, 8); v += __shfl_xor(v, 16);
+        if (lr == 0) sm.sum[32 * wave + (x & 3) + 8 * (x >> 2) + 4 * g2] = v;
+    }
+    __syncthreads();
+}
+
+// ---- fp32: the sums of at most 64 keys of this wave's rows, left in sm.sum ----
+template <int D>
+__device__ __forceinline__ void heavy_sums(WeightsSmem<float, D> &sm, const SpanArgs &a, const Seq &sq, const int32_t *table, int g, int j0,
+                                           int keys) {
+    constexpr int NT = D / 16;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, q = lane >> 4, base = sq.kv - sq.n;
+    const float c = a.scale_log2e;
+    f32x4_t kf[4][NT], sum[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const char *row = key_row(a, table, g, j0 + (16 * h + n < keys ? 16 * h + n : keys - 1));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) kf[h][t] = *reinterpret_cast<const f32x4_t *>(row + 64 * t + 16 * q);
+        sum[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    int R0, R1;
+    rows_of(a, sq, j0, j0 + keys - 1, &R0, &R1);
+    for (int R = R0 + 16 * wave; R < R1; R += 64) {
+        const int rr = R + n < R1 ? R + n : R1 - 1, t = token_of(a, rr), h0 = g * a.G + rr - t * a.G;
+        const char *row = (const char *)((const float *)a.Q + h0 * a.qs_h + (sq.q0 + t) * a.qs_t);
+        f32x4_t qf[NT];
+#pragma unroll
+        for (int u = 0; u < NT; ++u) qf[u] = *reinterpret_cast<const f32x4_t *>(row + 64 * u + 16 * q);
+        const float2 nm = a.norm[h0 * a.T + sq.q0 + t];
+        const int p = R + n < R1 ? base + t : -1;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][u][e], qf[u][e], x, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + 16 * h + 4 * q + i;
+                const float e = __builtin_amdgcn_exp2f(x[i] * c - nm.x) * nm.y;
+                sum[h][i] += j <= p && p < key_hi(a, j) ? e : 0.f;
+            }
+        }
+    }
+    __syncthreads();     // the sums of the share before have been read
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = sum[h][i];
+            x += __shfl_xor(x, 1); x += __shfl_xor(x, 2); x += __shfl_xor(x, 4); x += __shfl_xor(x, 8);
+            if (n == 0) sm.sum[wave][16 * h + 4 * q + i] = x;
+        }
+    __syncthreads();
+}
+
+template <int D> __device__ __forceinline__ float sum_of(const WeightsSmem<bf16_t, D> &sm, int k) { return sm.sum[k]; }
+template <int D> __device__ __forceinline__ float sum_of(const WeightsSmem<float, D> &sm, int k) {
+    return (sm.sum[0][k] + sm.sum[1][k]) + (sm.sum[2][k] + sm.sum[3][k]);
+}
 
 }  // namespace
 
-constexpr int kWKeys = 64;
-
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restrict__ W, float decay) {
-    typedef typename Frag<T>::type F;
-    constexpr int NT = D * (int)sizeof(T) / 64;
-    __shared__ float s_sum[4][kWKeys];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15, q = lane >> 4;
-    const float c = a.scale_log2e;
+    constexpr int KEYS = Heavy<T>::kKeys;
+    __shared__ WeightsSmem<T, D> sm;
+    const int tid = threadIdx.x, lane = tid & 63;
     for (unsigned b = blockIdx.x;; b += gridDim.x) {
-        // the item: as find_item, of key tiles
-        const int g = (int)(b % (unsigned)a.H_kv);
-        int want = (int)(b / (unsigned)a.H_kv), s = -1, tile = 0;
-        for (int s0 = 0, base = 0; s0 < a.n_seq; s0 += 64) {
-            int tiles = 0;
-            if (s0 + lane < a.n_seq) tiles = (read_seq(a, s0 + lane).kv + kWKeys - 1) / kWKeys;
+        // the share: as find_item, of key tiles
+        const int g = (int)(b % (unsigned)a.H_kv), want = (int)(b / (unsigned)a.H_kv);
+        int s = -1, tile = 0, units = 0, end_units = 0;
+        for (int s0 = 0, base = 0, before = 0; s0 < a.n_seq; s0 += 64) {
+            int tiles = 0, need = 0;
+            if (s0 + lane < a.n_seq) {
+                const Seq q = read_seq(a, s0 + lane);
+                need = score_need(a, q);
+                tiles = q.kv;
+            }
+            const int need_end = capped(before + wave_incl_scan(need));
+            const bool kept = need > 0 && need_end <= a.score_units;
+            tiles = kept ? (tiles + kKeptKeys - 1) / kKeptKeys : (tiles + KEYS - 1) / KEYS;
             const int end = wave_incl_scan(tiles), total = __builtin_amdgcn_readlane(end, 63);
             if (want < base + total) {
                 const int l = __builtin_ctzll(__ballot(want < base + end));
                 s = s0 + l;
                 tile = want - base - __builtin_amdgcn_readlane(end - tiles, l);
+                units = __builtin_amdgcn_readlane(kept ? need : 0, l);
+                end_units = __builtin_amdgcn_readlane(need_end, l);
                 break;
             }
             base += total;
+            before = __builtin_amdgcn_readlane(need_end, 63);
         }
         if (s < 0) return;
         const Seq sq = read_seq(a, s);
-        const int j0 = tile * kWKeys, base = sq.kv - sq.n;
-        const int keys = sq.kv - j0 < kWKeys ? sq.kv - j0 : kWKeys;
         const int32_t *table = a.table + (int64_t)s * a.max_pages;
-        const char *Kg = (const char *)a.K + g * a.ks_h;
-        F kf[4][NT];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int key = 16 * h + n < keys ? 16 * h + n : keys - 1, slot = j0 + key;
-            const int pi = page_of(a, slot);
-            int page = table[pi];
-            if ((unsigned)page >= (unsigned)a.n_pages) page = 0;
-            const char *row = Kg + ((uint64_t)((uint32_t)page * a.ks_p + (uint32_t)(slot - pi * a.page_size) * a.ks_s) << 4);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) kf[h][t] = *reinterpret_cast<const F *>(row + 64 * t + 16 * q);
+        if (units == 0) {
+            const int j0 = tile * KEYS, keys = sq.kv - j0 < KEYS ? sq.kv - j0 : KEYS;
+            heavy_sums<D>(sm, a, sq, table, g, j0, keys);
+            if (tid < keys) put_weight(a, table, g, j0 + tid, W, decay, sum_of<D>(sm, tid));
+            continue;
         }
-        f32x4_t sum[4];
+        // kept scores: row R of tile R / M has them in the order of the tile's span
+        const int row = (sq.kv + 63) >> 6 << 6, rows = sq.n * a.G, base = sq.kv - sq.n;
+        const float *from = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * rows * row;
+        const int j = tile * kKeptKeys + 4 * tid;
+        if (j < sq.kv) {
+            f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+            for (int R = 0; R < rows; ++R) {
+                const int t = token_of(a, R), R0 = R / a.M * a.M;
+                const int R_end = (R0 + a.M < rows ? R0 + a.M : rows) - 1;
+                const Span span = make_span(a, base + token_of(a, R0), base + token_of(a, R_end));
+                const float2 nm = a.norm[(int64_t)(g * a.G + R - t * a.G) * a.T + sq.q0 + t];
+                f32x4_t x;
+                if (span.lo == 0 && j + 3 < span.total) {
+                    x = *reinterpret_cast<const f32x4_t *>(from + (int64_t)R * row + j);
+                } else {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) sum[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        // the new tokens that may see one of the keys
-        const int t_lo = j0 > base ? j0 - base : 0;
-        const int far = key_hi(a, j0 + keys - 1);       // no position from here on sees the last key, unless it is ...
-        const int t_hi = j0 < a.sinks || far >= sq.kv ? sq.n : far - base;      // ... behind one that stays visible
-        const int64_t R1 = t_hi > t_lo ? (int64_t)t_hi * a.G : 0;
-        for (int64_t R0 = (int64_t)t_lo * a.G + 16 * wave; R0 < R1; R0 += 64) {
-            const int R = (int)(R0 + n < R1 ? R0 + n : R1 - 1), t = R / a.G, h0 = g * a.G + R % a.G;
-            const bool live = R0 + n < R1;
-            const char *row = (const char *)((const T *)a.Q + h0 * a.qs_h + (sq.q0 + t) * a.qs_t);
-            F qf[NT];
-#pragma unroll
-            for (int u = 0; u < NT; ++u) qf[u] = *reinterpret_cast<const F *>(row + 64 * u + 16 * q);
-            const float2 nm = a.norm[h0 * a.T + sq.q0 + t];
-            const int p = live ? base + t : -1;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int u = 0; u < NT; ++u) x = Frag<T>::mfma(kf[h][u], qf[u], x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + 16 * h + 4 * q + i;
-                    const float e = __builtin_amdgcn_exp2f(x[i] * c - nm.x) * nm.y;
-                    sum[h][i] += j <= p && p < key_hi(a, j) ? e : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = j + i < span.head ? j + i : j + i >= span.lo ? j + i - span.lo + span.head : kIntMaxP;
+                        x[i] = at < span.total ? from[(int64_t)R * row + at] : -INFINITY;
+                    }
                 }
-            }
-        }
-        __syncthreads();     // the sums of the share before have been read
 #pragma unroll
-        for (int h = 0; h < 4; ++h)
+                for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(x[i] - nm.x) * nm.y;
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x = sum[h][i];
-                x += __shfl_xor(x, 1); x += __shfl_xor(x, 2); x += __shfl_xor(x, 4); x += __shfl_xor(x, 8);
-                if (n == 0) s_sum[wave][16 * h + 4 * q + i] = x;
-            }
-        __syncthreads();
-        if (tid < keys) {
-            const int slot = j0 + tid, pi = page_of(a, slot), page = table[pi];
-            if ((unsigned)page < (unsigned)a.n_pages) {
-                float *w = W + ((int64_t)page * a.H_kv + g) * a.page_size + (slot - pi * a.page_size);
-                const float x = (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]);
-                *w = decay > 0.f ? decay * *w + x : x;
-            }
+            for (int i = 0; i < 4; ++i)
+                if (j + i < sq.kv) put_weight(a, table, g, j + i, W, decay, sum[i]);
         }
     }
 }

@@ -574,7 +574,7 @@ def test_captured_and_replayed():
 
 def test_refusals_on_the_device():
     b = Batch([(1, 20), (2, 30)], 4, 2, 64, BF16, 16)
-    ws, O = dhsa.alloc_paged(b.prob), torch.empty_like(b.Q)
+    ws, O = dhsa.alloc_paged(b.prob, weights=False), torch.empty_like(b.Q)
     good = dict(Q=b.Q, K=b.K, V=b.V, table=b.table, q_start=b.q_start, kv_len=b.kv_len, O=O, lse=None, weights=None)
     W = b.new_weights()
     for bad in (dict(Q=b.Q[:, :2]), dict(Q=b.Q.float()), dict(K=b.K[:-1]), dict(K=b.K.permute(0, 2, 1, 3)), dict(table=b.table.long()),

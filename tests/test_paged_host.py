@@ -92,7 +92,8 @@ def test_arguments_that_are_refused():
         assert attend(p, **{name: P + 8}) == ALIGN, name
     for decay in (-0.5, 1.5, float("nan")):
         assert attend(p, decay=decay) == SHAPE
-    assert attend(p, n=dhsa.dhsa_paged_workspace_bytes(p) - 1) == WORKSPACE
+    assert attend(p, n=dhsa.dhsa_paged_workspace_bytes(p, False) - 1) == WORKSPACE
+    assert attend(p, weights=P, n=dhsa.dhsa_paged_workspace_bytes(p) - 1) == WORKSPACE
     for name in ("Kn", "Vn", "K", "V", "table", "q_start", "kv_len"):
         assert append(p, **{name: None}) == NULL, name
     for name in ("Kn", "Vn", "K", "V"):
@@ -120,7 +121,13 @@ def test_nothing_to_do_needs_nothing():
 
 def test_sizes():
     a, b = prob(), prob(max_pages=1 << 16, n_pages=1 << 20)
-    assert dhsa.dhsa_paged_workspace_bytes(a) == dhsa.dhsa_paged_workspace_bytes(b) > 0      # not of the lengths
+    assert dhsa.dhsa_paged_workspace_bytes(a, False) == dhsa.dhsa_paged_workspace_bytes(b, False) > 0      # not of the lengths
+    c = prob(max_pages=64)
+    # kept scores: 10 tokens of 3 sequences, groups of four: 14 rows of a kv-head for each of the pool's slots
+    assert 4 * 14 * 2 * 16 * 40 <= dhsa.dhsa_paged_workspace_bytes(c) - dhsa.dhsa_paged_workspace_bytes(c, False) <= 4 * 14 * 2 * 16 * 40 + 40000
+    assert dhsa.dhsa_paged_workspace_bytes(b) <= dhsa.dhsa_paged_workspace_bytes(b, False) + (1 << 32) + 4096
+    many = prob(T=3000)
+    assert dhsa.dhsa_paged_workspace_bytes(many) - dhsa.dhsa_paged_workspace_bytes(many, False) <= 8 * 3000 * 8 + 256     # many tokens: none
     assert dhsa.dhsa_paged_evict_workspace_bytes(a, 100) >= 4 * 3 * 2 * 101
     # no more lists than there are slots
     assert dhsa.dhsa_paged_evict_workspace_bytes(a, 1 << 30) == dhsa.dhsa_paged_evict_workspace_bytes(a, 16 * 8)
