@@ -32,8 +32,8 @@ struct SpanArgs {
     int2 *cut;
     int g_shift;                 // R / G = R g_mul >> g_shift
     uint32_t g_mul;
-    // scores of sequences of at most kFewRows rows a kv-head, for the weights (nullptr: none are kept): score_units blocks of 64;
-    // a row has ceil(kv / 64) blocks, its packed keys in order
+    // scores of sequences of at most kFewRows rows a kv-head, for the weights (nullptr: none are kept): score_units times 64.  A
+    // kv-head of a sequence has 64 ceil(kv / 64) for each row, its packed keys in blocks of 32, the rows of a block side by side
     float *scores;
     int score_units;
 };
@@ -109,9 +109,9 @@ __device__ __forceinline__ float wave_sum(float x) {
 struct Item {
     Seq q;
     int s, g, R0, rows, piece, pieces, slot;
-    float *scores;   // of row R0, or nullptr
-    int score_row;   // from row to row
+    float *scores;   // of the kv-head, or nullptr
 };
+__device__ __forceinline__ int64_t score_at(int rows, int R, int x) { return ((int64_t)(x >> 5) * rows + R) * 32 + (x & 31); }
 
 // Which share workgroup b has, M rows a tile and U keys a unit.  Every wave finds out for itself, without a barrier: lane i
 // looks at sequence 64 r + i.  A sequence's tiles all have as many pieces as its longest one needs, so that a piece has at most
@@ -171,10 +171,9 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
             it->rows = left < M ? (int)left : M;
             it->slot = it->pieces > 1 ? (part + of(cut_end - cut) + at) * a.H_kv + g : -1;
             it->scores = nullptr;
-            it->score_row = (it->q.kv + 63) >> 6 << 6;
             const int units = of(need), end_units = capped(units_before + of(need_end));
             if (units > 0 && end_units <= a.score_units)
-                it->scores = a.scores + (int64_t)(end_units - units) * 64 + ((int64_t)g * it->q.n * a.G + it->R0) * it->score_row;
+                it->scores = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * it->q.n * a.G * ((it->q.kv + 63) >> 6 << 6);
             found = true;
         }
         units_before = capped(units_before + __builtin_amdgcn_readlane(need_end, 63));

@@ -199,18 +199,28 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 
     uint32_t *const koff = sm.li.k[wave], *const voff = sm.li.v[wave];
     const float c = a.scale_log2e;
-    for (int x = x_lo + wave * BK; x < x_hi; x += 4 * BK) {
-        // places of the block's rows; keys past the end repeat the last one
+    // this lane's key of the block at x; keys past the end repeat the last one
+    const auto slot_at = [&](int x) {
         const int xk = x + (lane & (BK - 1));
-        const int slot = span.slot(xk < x_hi ? xk : x_hi - 1);
-        bool bad = xk >= x_hi;
+        return span.slot(xk < x_hi ? xk : x_hi - 1);
+    };
+    const auto ask = [&](int x) { return PAGED && x < x_hi ? table[page_of(a, slot_at(x))] : 0; };
+    struct Block {
+        typename Tl::Keys kv;
+        unsigned long long bad;      // keys that are not there
+        bool masked;                 // some row of the tile does not see some key of the block
+    };
+    int page = ask(x_lo + wave * BK);     // asked for a block ahead: the answer does not wait behind the block in between
+    const auto fetch = [&](Block &b, int x) {
+        const int slot = slot_at(x);
+        bool bad = x + (lane & (BK - 1)) >= x_hi;
         uint32_t ko, vo;
         if constexpr (PAGED) {
-            const int pi = page_of(a, slot), in = slot - pi * a.page_size;
-            int page = table[pi];
+            const int in = slot - page_of(a, slot) * a.page_size;
             if ((unsigned)page >= (unsigned)a.n_pages) { bad = true; page = 0; }
             ko = (uint32_t)page * a.ks_p + (uint32_t)in * a.ks_s;
             vo = (uint32_t)page * a.vs_p + (uint32_t)in * a.vs_s;
+            page = ask(x + 4 * BK);
         } else {
             ko = (uint32_t)slot * a.ks_s;
             vo = (uint32_t)slot * a.vs_s;
@@ -219,31 +229,30 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
         // (a wave's LDS operations are executed in order: only the compiler has to keep them so)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        // does some row of the tile not see some key of the block?
-        const int hi_k = key_hi(a, slot);
-        const unsigned long long bad_m = __ballot(bad);
-        const bool masked = __any(bad || slot > p_lo || hi_k <= p_hi);
-        typename Tl::Keys kv;
-        Tl::load(kv, Kg, Vg, koff, voff, n, q);
-        if (PAGED && bad_m) Tl::clear(kv, bad_m, q);
+        b.bad = __ballot(bad);
+        b.masked = __any(bad || slot > p_lo || key_hi(a, slot) <= p_hi);
+        Tl::load(b.kv, Kg, Vg, koff, voff, n, q);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+    };
+    const auto step = [&](Block &b, int x) {
+        if (PAGED && b.bad) Tl::clear(b.kv, b.bad, q);
         float p[RB][NP];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             float s[NP];
-            tl.scores(kv, r, s);
-            if (masked) {
+            tl.scores(b.kv, r, s);
+            if (b.masked) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
                     const int key = 16 * (i >> 2) + 4 * q + (i & 3), j = span.slot(x + key);
-                    const bool sees = j <= pos[r] && pos[r] < key_hi(a, j) && !(bad_m >> key & 1);
+                    const bool sees = j <= pos[r] && pos[r] < key_hi(a, j) && !(b.bad >> key & 1);
                     s[i] = sees ? s[i] : -INFINITY;
                 }
             }
-            // (a block ends inside its row's share: the share is whole blocks of 64, pieces begin at multiples of 4 BK)
+            // (there is room for whole blocks, and pieces begin at multiples of 4 BK)
             if (it.scores && 16 * r + n < it.rows) {
-                float *to = it.scores + (int64_t)(16 * r + n) * it.score_row + x + 4 * q;
+                float *to = it.scores + score_at(it.q.n * a.G, it.R0 + 16 * r + n, x + 4 * q);
 #pragma unroll
                 for (int h = 0; h < NP / 4; ++h)
                     *reinterpret_cast<f32x4_t *>(to + 16 * h) = f32x4_t{s[4 * h] * c, s[4 * h + 1] * c, s[4 * h + 2] * c, s[4 * h + 3] * c};
@@ -270,7 +279,26 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tl.o[r][j][i] *= alpha;
         }
-        tl.add(kv, p);
+        tl.add(b.kv, p);
+    };
+    int x = x_lo + wave * BK;
+    if constexpr (RB == 1 || D == 64) {
+        // the next block is on its way while this one is worked on
+        Block b0, b1;
+        if (x < x_hi) fetch(b0, x);
+        for (; x < x_hi; x += 8 * BK) {
+            if (x + 4 * BK < x_hi) fetch(b1, x + 4 * BK);
+            step(b0, x);
+            if (x + 4 * BK >= x_hi) break;
+            if (x + 8 * BK < x_hi) fetch(b0, x + 8 * BK);
+            step(b1, x + 4 * BK);
+        }
+    } else {
+        Block b;         // (two would not fit the registers of two waves a SIMD)
+        for (; x < x_hi; x += 4 * BK) {
+            fetch(b, x);
+            step(b, x);
+        }
     }
 
     // ---- join the four waves ----

@@ -265,8 +265,8 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
             continue;
         }
         // kept scores: row R of tile R / M has them in the order of the tile's span
-        const int row = (sq.kv + 63) >> 6 << 6, rows = sq.n * a.G, base = sq.kv - sq.n;
-        const float *from = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * rows * row;
+        const int rows = sq.n * a.G, base = sq.kv - sq.n;
+        const float *from = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * rows * ((sq.kv + 63) >> 6 << 6);
         const int j = tile * kKeptKeys + 4 * tid;
         if (j < sq.kv) {
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
@@ -277,12 +277,12 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
                 const float2 nm = a.norm[(int64_t)(g * a.G + R - t * a.G) * a.T + sq.q0 + t];
                 f32x4_t x;
                 if (span.lo == 0 && j + 3 < span.total) {
-                    x = *reinterpret_cast<const f32x4_t *>(from + (int64_t)R * row + j);
+                    x = *reinterpret_cast<const f32x4_t *>(from + score_at(rows, R, j));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int at = j + i < span.head ? j + i : j + i >= span.lo ? j + i - span.lo + span.head : kIntMaxP;
-                        x[i] = at < span.total ? from[(int64_t)R * row + at] : -INFINITY;
+                        x[i] = at < span.total ? from[score_at(rows, R, at)] : -INFINITY;
                     }
                 }
 #pragma unroll
