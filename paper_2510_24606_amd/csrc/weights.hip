@@ -3,7 +3,7 @@
 // is made by one workgroup in a fixed order; nothing is added with atomics.
 //
 // A workgroup takes shares of two kinds, one after another:
-//   * 1024 keys of a kv-head of a sequence whose scores were kept (few rows): they are read, four keys a thread.
+//   * 4096 keys of a kv-head of a sequence whose scores were kept (few rows): they are read, four times four keys a thread.
 //   * otherwise the scores are made again from Q and K.  bf16: 128 keys, 32 in the registers of each wave, and the rows that see
 //     them staged through LDS in blocks of 64 (K from memory once, Q once per 128 keys).  S^T (keys x rows) = K Q^T, so a lane
 //     has 16 keys of one row: it adds up its own keys over its rows, and the 32 rows of a block follow once at the end.  Bound
@@ -20,7 +20,7 @@ namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kKeptKeys = 1024;
+constexpr int kKeptKeys = 4096;
 
 template <typename T> struct Heavy;
 template <> struct Heavy<bf16_t> { static constexpr int kKeys = 128, kRows = 64; };
@@ -267,31 +267,40 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
         // kept scores: row R of tile R / M has them in the order of the tile's span
         const int rows = sq.n * a.G, base = sq.kv - sq.n;
         const float *from = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * rows * ((sq.kv + 63) >> 6 << 6);
-        const int j = tile * kKeptKeys + 4 * tid;
-        if (j < sq.kv) {
-            f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-            for (int R = 0; R < rows; ++R) {
-                const int t = token_of(a, R), R0 = R / a.M * a.M;
-                const int R_end = (R0 + a.M < rows ? R0 + a.M : rows) - 1;
-                const Span span = make_span(a, base + token_of(a, R0), base + token_of(a, R_end));
-                const float2 nm = a.norm[(int64_t)(g * a.G + R - t * a.G) * a.T + sq.q0 + t];
-                f32x4_t x;
+        constexpr int U = kKeptKeys / 1024;
+        const int j0 = tile * kKeptKeys + 4 * tid;
+        f32x4_t sum[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int R = 0; R < rows; ++R) {
+            const int t = token_of(a, R), R0 = R / a.M * a.M;
+            const int R_end = (R0 + a.M < rows ? R0 + a.M : rows) - 1;
+            const Span span = make_span(a, base + token_of(a, R0), base + token_of(a, R_end));
+            const float2 nm = a.norm[(int64_t)(g * a.G + R - t * a.G) * a.T + sq.q0 + t];
+            f32x4_t x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + 1024 * u;
                 if (span.lo == 0 && j + 3 < span.total) {
-                    x = *reinterpret_cast<const f32x4_t *>(from + score_at(rows, R, j));
+                    x[u] = *reinterpret_cast<const f32x4_t *>(from + score_at(rows, R, j));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int at = j + i < span.head ? j + i : j + i >= span.lo ? j + i - span.lo + span.head : kIntMaxP;
-                        x[i] = at < span.total ? from[score_at(rows, R, at)] : -INFINITY;
+                        x[u][i] = at < span.total ? from[score_at(rows, R, at)] : -INFINITY;
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(x[i] - nm.x) * nm.y;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (j + i < sq.kv) put_weight(a, table, g, j + i, W, decay, sum[i]);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[u][i] += __builtin_amdgcn_exp2f(x[u][i] - nm.x) * nm.y;
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j0 + 1024 * u + i < sq.kv) put_weight(a, table, g, j0 + 1024 * u + i, W, decay, sum[u][i]);
     }
 }
 
