@@ -55,6 +55,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
 
+// A wave has consecutive slots, 64 at a time; IT times 1024 slots keep their keys in registers (what is longer reads them again).
+// 8 x 8 lists of up to 32768 slots: 83 us with the keys read five times, by page and slot each time.
+template <int IT>
 __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, EvictArgs e) {
     __shared__ int hist[2048];
     __shared__ int s_gt[kEvictWaves], s_eq[kEvictWaves], s_scan[kEvictWaves];
@@ -77,22 +80,40 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
     for (int x = tid; x < e.recent; x += kEvictThreads) put(e.keep - e.recent + x, m1 + x);
     if (need == 0) return;
     const int32_t *table = a.table + (int64_t)s * a.max_pages;
-    const auto key = [&](int slot) {
+    const int rounds = (m1 - m0 + kEvictThreads - 1) / kEvictThreads, w0 = m0 + wave * rounds * 64;
+    const auto read = [&](int slot) {
         const int pi = page_of(a, slot), page = table[pi];
         if ((unsigned)page >= (unsigned)a.n_pages) return 0u;
         return weight_key(e.weights[((int64_t)page * a.H_kv + g) * a.page_size + (slot - pi * a.page_size)]);
+    };
+    uint32_t held[IT];
+    if (rounds <= IT) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int x = w0 + 64 * i + lane;
+            held[i] = i < rounds ? read(x < m1 ? x : m1 - 1) : 0u;
+        }
+    }
+    // f(slot or -1, key) for every round of this wave
+    const auto each = [&](auto f) {
+        if (rounds <= IT) {
+#pragma unroll
+            for (int i = 0; i < IT; ++i)
+                if (i < rounds) { const int x = w0 + 64 * i + lane; f(x < m1 ? x : -1, held[i]); }
+        } else {
+            for (int i = 0; i < rounds; ++i) { const int x = w0 + 64 * i + lane; f(x < m1 ? x : -1, read(x < m1 ? x : m1 - 1)); }
+        }
     };
     // digits of 11, 11 and 10 bits
     uint32_t prefix = 0;
     int left = need;             // of the slots whose higher digits equal the prefix, how many stay
     for (int d = 0; d < 3; ++d) {
-        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
+        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048, above_shift = d == 2 ? 10 : 21;
         for (int x = tid; x < 2048; x += kEvictThreads) hist[x] = 0;
         __syncthreads();
-        for (int x = m0 + tid; x < m1; x += kEvictThreads) {
-            const uint32_t k = key(x);
-            if (d == 0 || k >> (shift + (d == 1 ? 11 : 10)) == prefix) atomicAdd(&hist[k >> shift & (bins - 1)], 1);
-        }
+        each([&](int x, uint32_t k) {
+            if (x >= 0 && (d == 0 || k >> above_shift == prefix)) atomicAdd(&hist[k >> shift & (bins - 1)], 1);
+        });
         __syncthreads();
         // thread i has the bins 2047 - 2 i and 2046 - 2 i: counts from the top down
         const int h1 = hist[2047 - 2 * tid], h0 = hist[2046 - 2 * tid];
@@ -100,51 +121,51 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
         if (lane == 63) s_scan[wave] = inc;
         __syncthreads();
         int above = inc - h0 - h1;
-        for (int w = 0; w < wave; ++w) above += s_scan[w];
+#pragma unroll
+        for (int w = 0; w < kEvictWaves; ++w) above += w < wave ? s_scan[w] : 0;
         if (above < left && left <= above + h1) { s_digit = 2047 - 2 * tid; s_left = left - above; }
         else if (above + h1 < left && left <= above + h1 + h0) { s_digit = 2046 - 2 * tid; s_left = left - above - h1; }
         __syncthreads();
         prefix = prefix << (d == 2 ? 10 : 11) | (uint32_t)s_digit;
         left = s_left;
     }
-    // the list: a wave has consecutive slots
-    const int len = m1 - m0, per = (len + kEvictThreads - 1) / kEvictThreads * 64;
-    const int w0 = m0 + wave * per, w1 = w0 + per < m1 ? w0 + per : m1;
     int gt = 0, eq = 0;
-    for (int x = w0 + lane; x < w1; x += 64) {
-        const uint32_t k = key(x);
-        gt += k > prefix;
-        eq += k == prefix;
-    }
+    each([&](int x, uint32_t k) {
+        gt += x >= 0 && k > prefix;
+        eq += x >= 0 && k == prefix;
+    });
     gt = __builtin_amdgcn_readlane(wave_incl_scan(gt), 63);
     eq = __builtin_amdgcn_readlane(wave_incl_scan(eq), 63);
     if (lane == 0) { s_gt[wave] = gt; s_eq[wave] = eq; }
     __syncthreads();
     int gt0 = 0, eq0 = 0;        // above and equal in the slots before
-    for (int w = 0; w < wave; ++w) { gt0 += s_gt[w]; eq0 += s_eq[w]; }
-    for (int x0 = w0; x0 < w1; x0 += 64) {
-        const int x = x0 + lane;
-        const uint32_t k = x < w1 ? key(x) : 0u;
-        const unsigned long long mg = __ballot(x < w1 && k > prefix), me = __ballot(x < w1 && k == prefix);
+#pragma unroll
+    for (int w = 0; w < kEvictWaves; ++w) {
+        gt0 += w < wave ? s_gt[w] : 0;
+        eq0 += w < wave ? s_eq[w] : 0;
+    }
+    each([&](int x, uint32_t k) {
+        const unsigned long long mg = __ballot(x >= 0 && k > prefix), me = __ballot(x >= 0 && k == prefix);
         const unsigned long long below = (1ull << lane) - 1ull;
         const int ge = gt0 + __popcll(mg & below), ee = eq0 + __popcll(me & below);
-        if (x < w1 && (k > prefix || (k == prefix && ee < left))) put(e.first + ge + (ee < left ? ee : left), x);
+        if (x >= 0 && (k > prefix || (k == prefix && ee < left))) put(e.first + ge + (ee < left ? ee : left), x);
         gt0 += __popcll(mg);
         eq0 += __popcll(me);
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------
-// Eviction, second launch: the rows move.  Kept slots ascend, so row t moves from a slot >= t; batches are read whole before
-// they are written, and a batch is written below everything that a later one reads: a workgroup does its columns of a head
-// in place.  blockIdx.x: part (K columns, V columns, weights), y: kv-head, z: sequence.
+// Eviction, second launch: the rows move.  In place one workgroup does its columns of a head: kept slots ascend, so row t moves
+// from a slot >= t; batches are read whole before they are written, and a batch is written below everything that a later one
+// reads.  Into other pages every batch has a workgroup of its own (8 x 8 heads, 4096 rows each: 100 us with one for all).
+// blockIdx.x: part (K columns, V columns, weights) and batch, y: kv-head, z: sequence.
 // ---------------------------------------------------------------------------
 constexpr int kMoveU = 4;
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 template <typename V>
 __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e, int s, int n, const int32_t *list, char *base, uint64_t p16,
-                                          uint64_t s16, int unit, int lanes, int width) {
+                                          uint64_t s16, int unit, int lanes, int width, int batch, int batches) {
     // lanes threads per row, width bytes each; strides in `unit` bytes
     const int tid = threadIdx.x, r = tid / lanes, c = tid % lanes * width, rows = kEvictThreads / lanes;
     const int32_t *table = a.table + (int64_t)s * a.max_pages, *table_out = e.table_out + (int64_t)s * a.max_pages;
@@ -153,7 +174,7 @@ __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e,
         if ((unsigned)page >= (unsigned)a.n_pages) return nullptr;
         return base + ((uint64_t)page * p16 + (uint64_t)(slot - pi * a.page_size) * s16) * unit + c;
     };
-    for (int t0 = 0; t0 < n; t0 += rows * kMoveU) {
+    for (int t0 = batch * rows * kMoveU; t0 < n; t0 += batches * rows * kMoveU) {
         V x[kMoveU];
         char *to[kMoveU];
 #pragma unroll
@@ -175,25 +196,31 @@ __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e,
 }
 
 __global__ __launch_bounds__(kEvictThreads) void k_evict_move(SpanArgs a, EvictArgs e, int row16, int parts) {
-    const int g = blockIdx.y, s = blockIdx.z, part = blockIdx.x;
+    const int g = blockIdx.y, s = blockIdx.z, part = blockIdx.x % (2 * parts + 1), batch = blockIdx.x / (2 * parts + 1);
+    const int batches = gridDim.x / (2 * parts + 1);
     const int64_t at = (int64_t)s * a.H_kv + g;
     const int n = e.count[at];
     const int32_t *list = e.list + at * e.stride;
     if (part == 2 * parts) {
-        move_rows<float>(a, e, s, n, list, (char *)(e.weights + (int64_t)g * a.page_size), (uint64_t)a.H_kv * a.page_size, 1, 4, 1, 4);
-        if (g == 0 && threadIdx.x == 0) e.kv_out[s] = n;      // (nothing of this launch reads kv_len)
+        move_rows<float>(a, e, s, n, list, (char *)(e.weights + (int64_t)g * a.page_size), (uint64_t)a.H_kv * a.page_size, 1, 4, 1, 4,
+                         batch, batches);
+        if (g == 0 && batch == 0 && threadIdx.x == 0) e.kv_out[s] = n;      // (nothing of this launch reads kv_len)
         return;
     }
     const bool is_k = part < parts;
     const int lanes = row16 / parts, c0 = (is_k ? part : part - parts) * lanes * 16;
     move_rows<u32x4_t>(a, e, s, n, list, (is_k ? e.K + g * a.ks_h : e.V + g * a.vs_h) + c0, is_k ? a.ks_p : a.vs_p, is_k ? a.ks_s : a.vs_s, 16,
-                     lanes, 16);
+                     lanes, 16, batch, batches);
 }
 
 hipError_t launch_evict(const SpanArgs &a, const EvictArgs &e, int row_bytes, hipStream_t s) {
     const int row16 = row_bytes / 16, parts = row16 / 8;      // 128 bytes a part
-    hipLaunchKernelGGL(k_evict_select, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
-    hipLaunchKernelGGL(k_evict_move, dim3(2 * parts + 1, a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e, row16, parts);
+    if (a.slots_max <= 4 * kEvictThreads) hipLaunchKernelGGL(k_evict_select<4>, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
+    else hipLaunchKernelGGL(k_evict_select<32>, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    const int per_batch = kEvictThreads / 8 * kMoveU, batches = e.table_out == a.table ? 1 : std::min(64, (e.stride + per_batch - 1) / per_batch);
+    hipLaunchKernelGGL(k_evict_move, dim3((2 * parts + 1) * batches, a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e, row16, parts);
     return hipGetLastError();
 }
 
