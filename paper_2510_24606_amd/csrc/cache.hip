@@ -163,11 +163,11 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
 constexpr int kMoveU = 4;
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-template <typename V>
+template <typename V, int THREADS>
 __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e, int s, int n, const int32_t *list, char *base, uint64_t p16,
                                           uint64_t s16, int unit, int lanes, int width, int batch, int batches) {
     // lanes threads per row, width bytes each; strides in `unit` bytes
-    const int tid = threadIdx.x, r = tid / lanes, c = tid % lanes * width, rows = kEvictThreads / lanes;
+    const int tid = threadIdx.x, r = tid / lanes, c = tid % lanes * width, rows = THREADS / lanes;
     const int32_t *table = a.table + (int64_t)s * a.max_pages, *table_out = e.table_out + (int64_t)s * a.max_pages;
     const auto place = [&](const int32_t *tb, int slot) -> char * {
         const int pi = page_of(a, slot), page = tb[pi];
@@ -187,40 +187,48 @@ __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e,
                 if (from) { x[u] = *reinterpret_cast<const V *>(from); to[u] = place(table_out, t); }
             }
         }
-        __syncthreads();
+        if constexpr (THREADS == kEvictThreads) __syncthreads();
 #pragma unroll
         for (int u = 0; u < kMoveU; ++u)
             if (to[u]) *reinterpret_cast<V *>(to[u]) = x[u];
-        __syncthreads();
+        if constexpr (THREADS == kEvictThreads) __syncthreads();
     }
 }
 
-__global__ __launch_bounds__(kEvictThreads) void k_evict_move(SpanArgs a, EvictArgs e, int row16, int parts) {
+// kEvictThreads: in place, one batch after another
+constexpr int kMoveThreads = 256;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_evict_move(SpanArgs a, EvictArgs e, int row16, int parts) {
     const int g = blockIdx.y, s = blockIdx.z, part = blockIdx.x % (2 * parts + 1), batch = blockIdx.x / (2 * parts + 1);
     const int batches = gridDim.x / (2 * parts + 1);
     const int64_t at = (int64_t)s * a.H_kv + g;
     const int n = e.count[at];
     const int32_t *list = e.list + at * e.stride;
     if (part == 2 * parts) {
-        move_rows<float>(a, e, s, n, list, (char *)(e.weights + (int64_t)g * a.page_size), (uint64_t)a.H_kv * a.page_size, 1, 4, 1, 4,
+        move_rows<float, THREADS>(a, e, s, n, list, (char *)(e.weights + (int64_t)g * a.page_size), (uint64_t)a.H_kv * a.page_size, 1, 4, 1, 4,
                          batch, batches);
         if (g == 0 && batch == 0 && threadIdx.x == 0) e.kv_out[s] = n;      // (nothing of this launch reads kv_len)
         return;
     }
     const bool is_k = part < parts;
     const int lanes = row16 / parts, c0 = (is_k ? part : part - parts) * lanes * 16;
-    move_rows<u32x4_t>(a, e, s, n, list, (is_k ? e.K + g * a.ks_h : e.V + g * a.vs_h) + c0, is_k ? a.ks_p : a.vs_p, is_k ? a.ks_s : a.vs_s, 16,
+    move_rows<u32x4_t, THREADS>(a, e, s, n, list, (is_k ? e.K + g * a.ks_h : e.V + g * a.vs_h) + c0, is_k ? a.ks_p : a.vs_p, is_k ? a.ks_s : a.vs_s, 16,
                      lanes, 16, batch, batches);
 }
 
 hipError_t launch_evict(const SpanArgs &a, const EvictArgs &e, int row_bytes, hipStream_t s) {
-    const int row16 = row_bytes / 16, parts = row16 / 8;      // 128 bytes a part
+    const int row16 = row_bytes / 16;
     if (a.slots_max <= 4 * kEvictThreads) hipLaunchKernelGGL(k_evict_select<4>, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
     else hipLaunchKernelGGL(k_evict_select<32>, dim3(a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const int per_batch = kEvictThreads / 8 * kMoveU, batches = e.table_out == a.table ? 1 : std::min(64, (e.stride + per_batch - 1) / per_batch);
-    hipLaunchKernelGGL(k_evict_move, dim3((2 * parts + 1) * batches, a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e, row16, parts);
+    if (e.table_out == a.table) {
+        const int parts = row16 / 8;      // 128 bytes a part: what is in order is the work of one workgroup each
+        hipLaunchKernelGGL(k_evict_move<kEvictThreads>, dim3(2 * parts + 1, a.H_kv, a.n_seq), dim3(kEvictThreads), 0, s, a, e, row16, parts);
+    } else {
+        const int64_t pieces = (int64_t)e.stride * row16, batches = std::min<int64_t>((pieces + kMoveThreads * kMoveU - 1) / (kMoveThreads * kMoveU), 256);
+        hipLaunchKernelGGL(k_evict_move<kMoveThreads>, dim3((unsigned)(3 * batches), a.H_kv, a.n_seq), dim3(kMoveThreads), 0, s, a, e, row16, 1);
+    }
     return hipGetLastError();
 }
 
