@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -120,11 +121,11 @@ def lib() -> C.CDLL:
         G = C.POINTER(dhsa_paged)
         l.dhsa_window_prefill.argtypes = [P, C.c_int64, C.c_int64, vp, vp, vp, vp, vp]
         l.dhsa_window_prefill.restype = C.c_int
-        l.dhsa_paged_append.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp]; l.dhsa_paged_append.restype = C.c_int
-        l.dhsa_paged_attend.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
+        l.dhsa_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]; l.dhsa_paged_append.restype = C.c_int
+        l.dhsa_paged_attend.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_float, vp, C.c_size_t, vp]
         l.dhsa_paged_attend.restype = C.c_int
         l.dhsa_paged_workspace_bytes.argtypes = [G, C.c_int]; l.dhsa_paged_workspace_bytes.restype = C.c_size_t
-        l.dhsa_paged_evict.argtypes = [G, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_size_t, vp]
+        l.dhsa_paged_evict.argtypes = [vp, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_size_t, vp]
         l.dhsa_paged_evict.restype = C.c_int
         l.dhsa_paged_evict_workspace_bytes.argtypes = [G, C.c_int32]; l.dhsa_paged_evict_workspace_bytes.restype = C.c_size_t
         l.dhsa_status_string.argtypes = [C.c_int]; l.dhsa_status_string.restype = C.c_char_p
@@ -367,24 +368,36 @@ def dhsa_decode_step(prob, Q, K, V, B, ws, N_c_cap: int, L_cap: int, kc_valid: i
 
 
 # ---- attention without routing: windows and paged caches ----
+# A step of a small batch takes the GPU a few microseconds: the checks of tensors against the problem are kept short.
 
-def _same(what: str, t, dtype, shape, contiguous: bool = False) -> None:
-    """The tensors of the calls below are described by one problem struct: what does not fit it is refused here."""
-    if t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, where {dtype} {shape} on the current device is wanted")
-    if not (t.is_contiguous() if contiguous else t.stride(-1) == 1 and 0 not in t.stride()):   # (a stride of 0 says packed)
-        raise ValueError(f"{what}: strides {t.stride()}: contiguous rows are wanted, none of them shared")
+def _same(what: str, t, dtype, shape, dev: int, strides=None):
+    """The tensors of the calls below are described by one problem struct: what does not fit it is refused here.  strides: what
+    they have to be, None: any of contiguous rows (a stride of 0 would say packed).  Returns them."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, where {dtype} {tuple(shape)} on the current device is wanted")
+    if st != strides if strides is not None else (st[-1] != 1 or 0 in st):
+        raise ValueError(f"{what}: strides {st}, where {strides or 'contiguous rows, none of them shared'} are wanted")
+    return st
 
 
 def dhsa_window_prefill(prob, Q, K, V, O, window: int, sinks: int = 0) -> None:
     """Causal attention of a prompt in which row i sees the keys j <= i with i - j < window or j < sinks.  prob: problem(Q, K,
     [0, L], L); its chunks and budget play no part."""
-    kv = (prob.H_kv, prob.L, prob.D)
-    _same("Q", Q, Q.dtype, (prob.H_q, prob.L, prob.D)); _same("O", O, Q.dtype, (prob.H_q, prob.L, prob.D))
-    _same("K", K, Q.dtype, kv); _same("V", V, Q.dtype, kv)
-    p = _with_vo(prob, V, O)
+    L, H_q, H_kv, D = prob.L, prob.H_q, prob.H_kv, prob.D
+    dev, dt, rows, kv = torch.cuda.current_device(), Q.dtype, (H_q, L, D), (H_kv, L, D)
+    p = dhsa_problem.from_buffer_copy(prob)
+    p.q_stride_h, p.q_stride_l, _ = _same("Q", Q, dt, rows, dev)
+    p.k_stride_h, p.k_stride_l, _ = _same("K", K, dt, kv, dev)
+    p.v_stride_h, p.v_stride_l, _ = _same("V", V, dt, kv, dev)
+    p.o_stride_h, p.o_stride_l, _ = _same("O", O, dt, rows, dev)
+    if _DTYPES.get(dt, -1) != prob.dtype:
+        raise ValueError(f"Q: {dt}, which is not the problem's type")
     _check(lib().dhsa_window_prefill(C.byref(p), window, sinks, Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
                                      _stream()))
+
+
+_PAGED = struct.Struct("@qiiiiiiiifqqqqqqqqqqqqqqqq")      # dhsa_paged: read and written at once
 
 
 def paged_problem(K, V, table, H_q: int, T: int, window: int = 0, sinks: int = 0, scale: float = 0.0) -> dhsa_paged:
@@ -421,61 +434,70 @@ def alloc_evict(prob: dhsa_paged, keep: int, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _same_cache(prob, K, V, table, weights) -> None:
-    pool = (prob.n_pages, prob.H_kv, prob.page_size, prob.D)
-    _same("K", K, K.dtype, pool); _same("V", V, K.dtype, pool)
-    if _DTYPES.get(K.dtype, -1) != prob.dtype or K.stride()[:3] != (prob.k_stride_p, prob.k_stride_h, prob.k_stride_s) or \
-            V.stride()[:3] != (prob.v_stride_p, prob.v_stride_h, prob.v_stride_s):
-        raise ValueError("K and V are not laid out as the problem says")
-    _same("table", table, torch.int32, (prob.n_seq, prob.max_pages), True)
+def _same_cache(f, K, V, table, weights, dev: int):
+    """K, V, the table and the weights against the fields of the problem; the strides of contiguous [n_pages, H_kv, page_size]."""
+    n_seq, H_kv, D, page, n_pages, width = f[1], f[3], f[4], f[6], f[7], f[8]
+    pool = (n_pages, H_kv, page, D)
+    _same("K", K, K.dtype, pool, dev, f[16:19] + (1,))
+    _same("V", V, K.dtype, pool, dev, f[19:22] + (1,))
+    if _DTYPES.get(K.dtype, -1) != f[5]:
+        raise ValueError(f"K: {K.dtype}, which is not the problem's type")
+    _same("table", table, torch.int32, (n_seq, width), dev, (width, 1))
     if weights is not None:
-        _same("weights", weights, torch.float32, pool[:3], True)
+        _same("weights", weights, torch.float32, pool[:3], dev, (H_kv * page, page, 1))
 
 
 def dhsa_paged_append(prob, K_new, V_new, K, V, table, q_start, kv_len, weights=None) -> None:
     """New rows K_new, V_new [H_kv, T, D] into the slots kv_len[s] - n_s .. kv_len[s] - 1 of their sequences; `weights` (float
     [n_pages, H_kv, page_size]) becomes 0 there."""
-    _same_cache(prob, K, V, table, weights)
-    new = (prob.H_kv, prob.T, prob.D)
-    _same("K_new", K_new, K.dtype, new); _same("V_new", V_new, K.dtype, new)
-    _same("q_start", q_start, torch.int32, (prob.n_seq + 1,), True); _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True)
-    p = dhsa_paged.from_buffer_copy(prob)
-    p.kn_stride_h, p.kn_stride_t = K_new.stride()[:2]
-    p.vn_stride_h, p.vn_stride_t = V_new.stride()[:2]
-    _check(lib().dhsa_paged_append(C.byref(p), K_new.data_ptr(), V_new.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(),
-                                   q_start.data_ptr(), kv_len.data_ptr(), None if weights is None else weights.data_ptr(),
-                                   _stream()))
+    f = _PAGED.unpack_from(prob)
+    dev, n_seq, new = torch.cuda.current_device(), f[1], (f[3], f[0], f[4])
+    _same_cache(f, K, V, table, weights, dev)
+    k = _same("K_new", K_new, K.dtype, new, dev)
+    v = _same("V_new", V_new, K.dtype, new, dev)
+    _same("q_start", q_start, torch.int32, (n_seq + 1,), dev, (1,))
+    _same("kv_len", kv_len, torch.int32, (n_seq,), dev, (1,))
+    _check(lib().dhsa_paged_append(_PAGED.pack(*f[:22], k[0], k[1], v[0], v[1]), K_new.data_ptr(), V_new.data_ptr(), K.data_ptr(),
+                                   V.data_ptr(), table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
+                                   None if weights is None else weights.data_ptr(), _stream()))
 
 
 def dhsa_paged_attend(prob, Q, K, V, table, q_start, kv_len, O, ws, lse=None, weights=None, decay: float = 1.0) -> None:
     """Attention of the new tokens Q [H_q, T, D] over the cache, their own rows included: O like Q, lse float [H_q, T].
     weights (float [n_pages, H_kv, page_size]) = decay weights + what each cached key got from this call's rows and heads."""
-    _same_cache(prob, K, V, table, weights)
-    rows = (prob.H_q, prob.T, prob.D)
-    _same("Q", Q, K.dtype, rows); _same("O", O, K.dtype, rows)
-    _same("q_start", q_start, torch.int32, (prob.n_seq + 1,), True); _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True)
+    f = _PAGED.unpack_from(prob)
+    dev, T, n_seq, H_q = torch.cuda.current_device(), f[0], f[1], f[2]
+    rows = (H_q, T, f[4])
+    _same_cache(f, K, V, table, weights, dev)
+    q = _same("Q", Q, K.dtype, rows, dev)
+    o = _same("O", O, K.dtype, rows, dev)
+    _same("q_start", q_start, torch.int32, (n_seq + 1,), dev, (1,))
+    _same("kv_len", kv_len, torch.int32, (n_seq,), dev, (1,))
     if lse is not None:
-        _same("lse", lse, torch.float32, rows[:2], True)
-    p = dhsa_paged.from_buffer_copy(prob)
-    p.q_stride_h, p.q_stride_t = Q.stride()[:2]
-    p.o_stride_h, p.o_stride_t = O.stride()[:2]
-    _check(lib().dhsa_paged_attend(C.byref(p), Q.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(), q_start.data_ptr(),
-                                   kv_len.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(),
-                                   None if weights is None else weights.data_ptr(), decay, ws.data_ptr(), ws.numel(), _stream()))
+        _same("lse", lse, torch.float32, (H_q, T), dev, (max(T, 1), 1))
+    _check(lib().dhsa_paged_attend(_PAGED.pack(*f[:12], q[0], q[1], o[0], o[1], *f[16:]), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+                                   table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), O.data_ptr(),
+                                   None if lse is None else lse.data_ptr(), None if weights is None else weights.data_ptr(), decay,
+                                   ws.data_ptr(), ws.numel(), _stream()))
 
 
 def dhsa_paged_evict(prob, K, V, weights, table, kv_len, keep: int, first: int, recent: int, ws, kv_len_out, table_out=None,
                      idx=None) -> None:
     """Cut every sequence down to `keep` tokens: of each kv-head the first ones, the `recent` last ones and the heaviest others
     stay and move to the front, in place or into the pages of table_out.  idx: int32 [n_seq, H_kv, keep], the slots that stayed."""
-    _same_cache(prob, K, V, table, weights)
-    _same("kv_len", kv_len, torch.int32, (prob.n_seq,), True); _same("kv_len_out", kv_len_out, torch.int32, (prob.n_seq,), True)
-    if table_out is not None:
-        _same("table_out", table_out, torch.int32, (prob.n_seq, prob.max_pages), True)
+    f = _PAGED.unpack_from(prob)
+    dev, n_seq, H_kv, width = torch.cuda.current_device(), f[1], f[3], f[8]
+    _same_cache(f, K, V, table, weights, dev)
+    _same("kv_len", kv_len, torch.int32, (n_seq,), dev, (1,))
+    _same("kv_len_out", kv_len_out, torch.int32, (n_seq,), dev, (1,))
+    if table_out is None:
+        table_out = table
+    else:
+        _same("table_out", table_out, torch.int32, (n_seq, width), dev, (width, 1))
     if idx is not None:
-        _same("idx", idx, torch.int32, (prob.n_seq, prob.H_kv, keep), True)
-    _check(lib().dhsa_paged_evict(C.byref(prob), K.data_ptr(), V.data_ptr(), weights.data_ptr(), table.data_ptr(), kv_len.data_ptr(),
-                                  keep, first, recent, (table if table_out is None else table_out).data_ptr(), kv_len_out.data_ptr(),
+        _same("idx", idx, torch.int32, (n_seq, H_kv, keep), dev, (H_kv * keep, keep, 1))
+    _check(lib().dhsa_paged_evict(_PAGED.pack(*f), K.data_ptr(), V.data_ptr(), weights.data_ptr(), table.data_ptr(), kv_len.data_ptr(),
+                                  keep, first, recent, table_out.data_ptr(), kv_len_out.data_ptr(),
                                   None if idx is None else idx.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
 
 
