@@ -21,6 +21,7 @@ namespace {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kKeptKeys = 4096;
+constexpr int kStages = 3;       // of 64 rows in LDS: two are on their way while one is worked on
 
 template <typename T> struct Heavy;
 template <> struct Heavy<bf16_t> { static constexpr int kKeys = 128, kRows = 64; };
@@ -28,9 +29,8 @@ template <> struct Heavy<float> { static constexpr int kKeys = 64, kRows = 16; }
 
 template <typename T, int D> struct WeightsSmem;
 template <int D> struct WeightsSmem<bf16_t, D> {
-    alignas(1024) uint16_t q[2][64 * D];
-    float2 norm[2][64];
-    int pos[2][64];
+    alignas(1024) uint16_t q[kStages][64 * D];
+    float norm[kStages][4][64];      // references, 1 / sums, and what the other two waves load beside their rows
     float sum[128];
 };
 template <int D> struct WeightsSmem<float, D> {
@@ -61,6 +61,18 @@ __device__ __forceinline__ void load16_to_lds(uint64_t addr, unsigned lds_window
     (void)addr; (void)lds_window;
 #endif
 }
+__device__ __forceinline__ void load4_to_lds(uint64_t addr, unsigned lds_window) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(addr), "s"(lds_window) : "memory");
+#else
+    (void)addr; (void)lds_window;
+#endif
+}
+template <int N> __device__ __forceinline__ void wait_loads() {      // all but the last N of this wave have landed
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+#endif
+}
 
 // byte address of row j of K of kv-head g (a page that is none: page 0, whose sums are not written)
 __device__ __forceinline__ const char *key_row(const SpanArgs &a, const int32_t *table, int g, int j) {
@@ -81,51 +93,43 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const Spa
     int R0, R1;
     rows_of(a, sq, j0, j0 + keys - 1, &R0, &R1);
     const int kw = j0 + 32 * wave;                     // this wave's first key
-    bf16x8 kf[NS];
-    {
-        const char *row = key_row(a, table, g, kw + lr < j0 + keys ? kw + lr : j0 + keys - 1) + 16 * g2;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) kf[s] = *reinterpret_cast<const bf16x8 *>(row + 32 * s);
-    }
-    // staging: load i of a wave fills the KiB 4 i + wave of the stage; pieces of a row are swizzled as in span_tall.hip
-    const int ld_row0 = wave * RPW + lane / OPR;
-    const unsigned ld_piece = 16u * ((lane % OPR) ^ piece_swizzle(ld_row0, OPR));
-    const unsigned lds_q = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)sm.q;
-    const int q_sw = piece_swizzle(lr, OPR);
-    const uint16_t *Qg = (const uint16_t *)a.Q + (int64_t)g * a.G * a.qs_h + sq.q0 * a.qs_t;
-    const auto ask = [&](int R, int buf) {
-#pragma unroll
-        for (int i = 0; i < LPS; ++i) {
-            const int r = R + ld_row0 + 4 * RPW * i, rr = r < R1 ? r : R1 - 1, t = token_of(a, rr), h = rr - t * a.G;
-            load16_to_lds((uint64_t)(uintptr_t)(Qg + h * a.qs_h + t * a.qs_t) + ld_piece, lds_q + buf * 128 * D + wave * 1024 + 4096 * i);
-        }
-    };
-    float2 nm;
-    int nt;
-    const auto ask_norm = [&](int R) {                 // threads 0 .. 63; a row that is not there gets p = 0
-        const int r = R + lane, rr = r < R1 ? r : R1 - 1;
-        nt = token_of(a, rr);
-        nm = a.norm[(int64_t)(g * a.G + rr - nt * a.G) * a.T + sq.q0 + nt];
-        if (r >= R1) nm = make_float2(1e30f, 0.f);
-    };
-    const auto put_norm = [&](int buf) { sm.norm[buf][lane] = nm; sm.pos[buf][lane] = base + nt; };
-
     f32x16 sum;
 #pragma unroll
     for (int x = 0; x < 16; ++x) sum[x] = 0.f;
     __syncthreads();                                   // the stages and sums of the share before have been read
     if (R0 < R1) {
-        ask(R0, 0);
-        if (wave == 0) { ask_norm(R0); put_norm(0); }
-        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0)
-        __syncthreads();
-        const int k_last = kw + 31 < sq.kv ? kw + 31 : sq.kv - 1, k_far = kw < a.sinks && k_last < a.sinks ? kIntMaxP : key_hi(a, kw < a.sinks ? a.sinks : kw);
-        for (int R = R0, buf = 0; R < R1; R += 64, buf ^= 1) {
-            const bool more = R + 64 < R1;
-            if (more) {
-                ask(R + 64, buf ^ 1);
-                if (wave == 0) ask_norm(R + 64);
+        bf16x8 kf[NS];
+        {
+            const char *row = key_row(a, table, g, kw + lr < j0 + keys ? kw + lr : j0 + keys - 1) + 16 * g2;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) kf[s] = *reinterpret_cast<const bf16x8 *>(row + 32 * s);
+        }
+        // Staging: load i of a wave fills the KiB 4 i + wave of the stage; pieces of a row are swizzled as in span_tall.hip.  Wave 0
+        // also loads the rows' references, wave 1 their 1 / sums, the others something, so that all wait for the same number.
+        const int ld_row0 = wave * RPW + lane / OPR;
+        const unsigned ld_piece = 16u * ((lane % OPR) ^ piece_swizzle(ld_row0, OPR));
+        const unsigned lds_q = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)sm.q;
+        const unsigned lds_n = (unsigned)(uintptr_t)(__attribute__((address_space(3))) float *)sm.norm;
+        const uint64_t Qg = (uint64_t)(uintptr_t)((const uint16_t *)a.Q + (int64_t)g * a.G * a.qs_h + sq.q0 * a.qs_t) + ld_piece;
+        const uint64_t Ng = (uint64_t)(uintptr_t)(a.norm + (int64_t)g * a.G * a.T + sq.q0) + (wave == 1 ? 4 : 0);
+        const auto ask = [&](int R, int buf) {         // rows from R on (behind the last one: that one again)
+#pragma unroll
+            for (int i = 0; i < LPS; ++i) {
+                const int r = R + ld_row0 + 4 * RPW * i, rr = r < R1 ? r : R1 - 1, t = token_of(a, rr), h = rr - t * a.G;
+                load16_to_lds(Qg + 2 * (h * a.qs_h + t * a.qs_t), lds_q + buf * 128 * D + wave * 1024 + 4096 * i);
             }
+            const int rr = R + lane < R1 ? R + lane : R1 - 1, t = token_of(a, rr), h = rr - t * a.G;
+            load4_to_lds(Ng + 8 * (h * a.T + t), lds_n + (buf * 4 + wave) * 256);
+        };
+        ask(R0, 0);
+        ask(R0 + 64, 1);
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0), in words that the compiler counts too: the keys are there
+        __syncthreads();
+        const int q_sw = piece_swizzle(lr, OPR);
+        const int k_last = kw + 31 < sq.kv ? kw + 31 : sq.kv - 1;
+        const int k_far = kw < a.sinks && k_last < a.sinks ? kIntMaxP : key_hi(a, kw < a.sinks ? a.sinks : kw);
+        for (int R = R0, buf = 0; R < R1; R += 64, buf = buf == kStages - 1 ? 0 : buf + 1) {
+            ask(R + 128, buf == 0 ? kStages - 1 : buf - 1);
             // do all rows of the stage see all keys of the wave?
             const int p0 = base + token_of(a, R), p1 = base + token_of(a, R + 63 < R1 ? R + 63 : R1 - 1);
             const bool masked = k_last > p0 || k_far <= p1;
@@ -138,9 +142,9 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const Spa
 #pragma unroll
                 for (int s = 0; s < NS; ++s)
                     s_ = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], *reinterpret_cast<const bf16x8 *>(qp + 16 * ((2 * s + g2) ^ q_sw)), s_, 0, 0, 0);
-                const float2 row = sm.norm[buf][rb * 32 + lr];
+                const float ref = sm.norm[buf][0][rb * 32 + lr], inv = R + rb * 32 + lr < R1 ? sm.norm[buf][1][rb * 32 + lr] : 0.f;
                 if (masked) {
-                    const int p = sm.pos[buf][rb * 32 + lr];
+                    const int p = base + token_of(a, R + rb * 32 + lr < R1 ? R + rb * 32 + lr : R1 - 1);
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
                         const int j = kw + (x & 3) + 8 * (x >> 2) + 4 * g2;
@@ -148,12 +152,12 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const Spa
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < 16; ++x) sum[x] += __builtin_amdgcn_exp2f(s_[x] * c - row.x) * row.y;
+                for (int x = 0; x < 16; ++x) sum[x] += __builtin_amdgcn_exp2f(s_[x] * c - ref) * inv;
             }
-            if (more && wave == 0) put_norm(buf ^ 1);
-            __builtin_amdgcn_s_waitcnt(0x0f70);
+            wait_loads<LPS + 1>();                     // of the next stage; those of the one behind it may be on their way
             __syncthreads();
         }
+        wait_loads<0>();
     }
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
@@ -305,7 +309,12 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
 }
 
 hipError_t launch_weights(const SpanArgs &a, int D, int dtype, float *W, float decay, hipStream_t s) {
-    const dim3 grid(1024);
+    // One workgroup a share where the pool's slots are in one sequence each (they take further ones where they are not): shares differ
+    // by how many rows see their keys, and the chip hands out workgroups as others end.  Chunks of 1..1024 tokens of 12 sequences, 1024
+    // workgroups with every 1024th share 358 us.
+    const int64_t keys = a.scores ? kKeptKeys : dtype == DHSA_F32 ? Heavy<float>::kKeys : Heavy<bf16_t>::kKeys;
+    const int64_t shares = ((int64_t)a.n_pages * a.page_size / keys + a.n_seq) * a.H_kv;
+    const dim3 grid((unsigned)std::min<int64_t>(shares, a.scores ? 1024 : 1 << 16));
     if (dtype == DHSA_F32) {
         if (D == 64) hipLaunchKernelGGL((k_weights<float, 64>), grid, dim3(256), 0, s, a, W, decay);
         else hipLaunchKernelGGL((k_weights<float, 128>), grid, dim3(256), 0, s, a, W, decay);
