@@ -456,10 +456,18 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
     }
 }
 
+// Rows of a tile, us of the two sides.
+// bf16, paged (K and V pass once a tile): 128 rows from 17 rows a kv-head and sequence on; of 32 rows, 16 sequences of 4096 tokens,
+// 32-row tiles 64 and 128-row tiles 44; one of 32768 37 and 24; of 36 rows 88 and 45.  Up to 16 rows the few wide loads of 16-row
+// tiles keep the memory busy.
+// bf16, one prompt: 128 rows from 144 tiles on: 2000 tokens, 8 heads of 2 kv-heads (125 tiles), a window of 2000 36 with smaller
+// tiles, 44 with 128 rows; 3500 tokens, a window of 300 26 and 17.
+// Else 32 rows, if they make 320 tiles: fp32, 4 heads of 64, a window of 256, 1021 tokens 16 rows 9.9 and 32 rows 13.6; 4000 tokens
+// 24.8 and 22.
 void choose_tiles(SpanArgs *a, int dtype, bool paged) {
     const int64_t rows = a->T * a->G, mean = rows / std::max(a->n_seq, 1);
-    a->M = mean > 16 ? 32 : 16;
-    if (dtype == DHSA_BF16 && mean > 48 && (paged || rows * a->H_kv >= 256 * kTallRows)) a->M = kTallRows;
+    a->M = mean > 16 && (paged || rows * a->H_kv >= 320 * 32) ? 32 : 16;
+    if (dtype == DHSA_BF16 && mean > 16 && (paged || rows * a->H_kv >= 144 * kTallRows)) a->M = kTallRows;
     a->target = !paged ? 0 : a->M == kTallRows ? 512 : 1024;
     a->part_cap = paged ? 2 * a->target + a->H_kv : 0;
 }
@@ -470,11 +478,10 @@ hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
     const int64_t blocks = (tiles + (a.target + a.H_kv - 1) / a.H_kv) * a.H_kv;
     for (int64_t b0 = 0; b0 < blocks; b0 += kGridMax) {
         const dim3 grid((unsigned)std::min<int64_t>(blocks - b0, kGridMax));
+#define DHSA_SPAN3(T_, D_, RB, PAGED) hipLaunchKernelGGL((k_span<T_, D_, RB, PAGED>), grid, dim3(256), 0, s, a, (unsigned)b0)
+// (bf16 has no paged tiles of 32 rows)
 #define DHSA_SPAN2(T_, D_, RB) \
-    do { \
-        if (a.table) hipLaunchKernelGGL((k_span<T_, D_, RB, true>), grid, dim3(256), 0, s, a, (unsigned)b0); \
-        else hipLaunchKernelGGL((k_span<T_, D_, RB, false>), grid, dim3(256), 0, s, a, (unsigned)b0); \
-    } while (0)
+    do { if (a.table) DHSA_SPAN3(T_, D_, (sizeof(T_) == 2 ? 1 : RB), true); else DHSA_SPAN3(T_, D_, RB, false); } while (0)
 #define DHSA_SPAN1(T_, D_) do { if (M == 16) DHSA_SPAN2(T_, D_, 1); else DHSA_SPAN2(T_, D_, 2); } while (0)
         if (M == kTallRows) {
             const hipError_t e = launch_span_tall(a, D, grid.x, (unsigned)b0, s);
@@ -485,6 +492,7 @@ hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
         else { if (D == 64) DHSA_SPAN1(bf16_t, 64); else DHSA_SPAN1(bf16_t, 128); }
 #undef DHSA_SPAN1
 #undef DHSA_SPAN2
+#undef DHSA_SPAN3
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
