@@ -403,6 +403,8 @@ typedef struct {
     int64_t vn_stride_h, vn_stride_t;
 } dhsa_paged;
 
+/* (Pointers to int32 and float arrays are 4-byte aligned, K, V, Q, O and workspaces 16-byte aligned.) */
+
 /* New rows into the cache: row t of sequence s goes to slot kv_len[s] - n_s + (t - q_start[s]).
  * weights_dev (may be NULL): set to 0 for those slots (see dhsa_paged_attend). */
 dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, const void *V_new_dev, void *K_dev,
@@ -435,7 +437,7 @@ size_t dhsa_paged_workspace_bytes(const dhsa_paged *prob, int weights);   /* 0 o
  * not in table_dev (the old pages are left as they were; shorter sequences move whole).  T, Q and
  * window play no part.  kv_len_out_dev: int32 [n_seq], min(kv_len, keep); may be kv_len_dev.
  * idx_dev (may be NULL): int32 [n_seq][H_kv][keep], the slots that stayed, ascending, -1 behind.
- * keep >= 1, first >= 0, recent >= 0, first + recent <= keep (else DHSA_ERR_BUDGET).  K rows are
+ * 1 <= keep <= 2^30, first >= 0, recent >= 0, first + recent <= keep (else DHSA_ERR_BUDGET).  K rows are
  * moved as they are: a rotary position stays the token's own, while a window counts slots.
  * ws_dev: scratch of dhsa_paged_evict_workspace_bytes(prob, keep) bytes, as above. */
 dhsa_status dhsa_paged_evict(const dhsa_paged *prob, void *K_dev, void *V_dev, float *weights_dev,

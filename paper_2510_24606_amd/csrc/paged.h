@@ -158,6 +158,7 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         if (want < base + total) {
             const int from = base + end - np;
             const unsigned long long hit = __ballot(want >= from && want < base + end);
+            if (hit == 0) return false;      // (arrays that are no sequences, whose tiles overflow)
             const int l = __builtin_ctzll(hit);
             const auto of = [l](int x) { return __builtin_amdgcn_readlane(x, l); };
             it->s = s0 + l;

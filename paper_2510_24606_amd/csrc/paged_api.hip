@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "paged.h"
 
@@ -14,6 +15,11 @@ namespace {
 #define DHSA_API __attribute__((visibility("default")))
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool odd_words(std::initializer_list<const void *> all) {
+    for (const void *p : all)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return true;
+    return false;
+}
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
 // x / d as a multiplication: with l = ceil(log2 d) and mul = floor(2^(31 + l) / d) + 1 < 2^32, mul d - 2^(31 + l) is
@@ -157,7 +163,9 @@ DHSA_API dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new
     if (st != DHSA_OK) return st;
     if (a.n_seq == 0 || a.T == 0) return DHSA_OK;
     if (!K_new_dev || !V_new_dev || !K_dev || !V_dev || !table_dev || !q_start_dev || !kv_len_dev) return DHSA_ERR_NULL;
-    if (misaligned(K_new_dev) || misaligned(V_new_dev) || misaligned(K_dev) || misaligned(V_dev)) return DHSA_ERR_ALIGN;
+    if (misaligned(K_new_dev) || misaligned(V_new_dev) || misaligned(K_dev) || misaligned(V_dev) ||
+        odd_words({table_dev, q_start_dev, kv_len_dev, weights_dev}))
+        return DHSA_ERR_ALIGN;
     a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev;
     ap.Kn = (const char *)K_new_dev; ap.Vn = (const char *)V_new_dev; ap.K = (char *)K_dev; ap.V = (char *)V_dev;
     ap.weights = weights_dev;
@@ -181,7 +189,9 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
     if (a.n_seq == 0 || (a.T == 0 && !weights_dev)) return DHSA_OK;
     if ((a.T > 0 && (!Q_dev || !O_dev)) || !K_dev || !V_dev || !table_dev || !q_start_dev || !kv_len_dev || !ws_dev)
         return DHSA_ERR_NULL;
-    if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(ws_dev)) return DHSA_ERR_ALIGN;
+    if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev) || misaligned(ws_dev) ||
+        odd_words({table_dev, q_start_dev, kv_len_dev, lse_dev, weights_dev}))
+        return DHSA_ERR_ALIGN;
     const PagedWs w = paged_ws(&a, prob->D, prob->dtype, weights_dev != nullptr);
     if (ws_bytes < (size_t)w.bytes) return DHSA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(ws_dev);
@@ -200,7 +210,7 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
 
 DHSA_API size_t dhsa_paged_evict_workspace_bytes(const dhsa_paged *prob, int32_t keep) {
     SpanArgs a;
-    if (resolve_paged(prob, &a, nullptr) != DHSA_OK || keep < 1) return 0;
+    if (resolve_paged(prob, &a, nullptr) != DHSA_OK || keep < 1 || keep > 1 << 30) return 0;
     const int64_t lists = (int64_t)std::max(a.n_seq, 1) * a.H_kv;
     return (size_t)(up256(lists * 4) + up256(lists * std::min<int64_t>(keep, a.slots_max) * 4));
 }
@@ -212,11 +222,13 @@ DHSA_API dhsa_status dhsa_paged_evict(const dhsa_paged *prob, void *K_dev, void 
     SpanArgs a;
     const dhsa_status st = resolve_paged(prob, &a, nullptr);
     if (st != DHSA_OK) return st;
-    if (keep < 1 || first < 0 || recent < 0 || (int64_t)first + recent > keep) return DHSA_ERR_BUDGET;
+    if (keep < 1 || keep > 1 << 30 || first < 0 || recent < 0 || (int64_t)first + recent > keep) return DHSA_ERR_BUDGET;
     if (a.n_seq == 0) return DHSA_OK;
     if (!K_dev || !V_dev || !weights_dev || !table_dev || !kv_len_dev || !table_out_dev || !kv_len_out_dev || !ws_dev)
         return DHSA_ERR_NULL;
-    if (misaligned(K_dev) || misaligned(V_dev) || misaligned(ws_dev)) return DHSA_ERR_ALIGN;
+    if (misaligned(K_dev) || misaligned(V_dev) || misaligned(ws_dev) ||
+        odd_words({table_dev, kv_len_dev, table_out_dev, kv_len_out_dev, idx_dev, weights_dev}))
+        return DHSA_ERR_ALIGN;
     if (ws_bytes < dhsa_paged_evict_workspace_bytes(prob, keep)) return DHSA_ERR_WORKSPACE;
     a.table = table_dev; a.kv_len = kv_len_dev;
     EvictArgs e;

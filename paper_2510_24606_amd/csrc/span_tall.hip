@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
     __shared__ Smem sm;
     Item it;
     if (!find_item(a, block0 + blockIdx.x, kTallRows, kTallKeys, &it)) return;
-    if (it.pieces > 1 && it.slot >= a.part_cap) return;      // (there are never so many)
+    if (it.pieces > 1 && (unsigned)it.slot >= (unsigned)a.part_cap) return;      // (there are never so many)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 31, g2 = lane >> 5;
     const int base = it.q.kv - it.q.n;                       // position of the first new token

@@ -233,11 +233,13 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
     constexpr int KEYS = Heavy<T>::kKeys;
     __shared__ WeightsSmem<T, D> sm;
     const int tid = threadIdx.x, lane = tid & 63;
-    for (unsigned b = blockIdx.x;; b += gridDim.x) {
+    for (uint64_t b = blockIdx.x;; b += gridDim.x) {      // (sequences may share pages: their tiles together may pass 32 bits)
         // the share: as find_item, of key tiles
-        const int g = (int)(b % (unsigned)a.H_kv), want = (int)(b / (unsigned)a.H_kv);
-        int s = -1, tile = 0, units = 0, end_units = 0;
-        for (int s0 = 0, base = 0, before = 0; s0 < a.n_seq; s0 += 64) {
+        const int g = (int)(b % (unsigned)a.H_kv);
+        const int64_t want = (int64_t)(b / (unsigned)a.H_kv);
+        int s = -1, tile = 0, units = 0, end_units = 0, before = 0;
+        int64_t seen = 0;
+        for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
             int tiles = 0, need = 0;
             if (s0 + lane < a.n_seq) {
                 const Seq q = read_seq(a, s0 + lane);
@@ -248,15 +250,15 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
             const bool kept = need > 0 && need_end <= a.score_units;
             tiles = kept ? (tiles + kKeptKeys - 1) / kKeptKeys : (tiles + KEYS - 1) / KEYS;
             const int end = wave_incl_scan(tiles), total = __builtin_amdgcn_readlane(end, 63);
-            if (want < base + total) {
-                const int l = __builtin_ctzll(__ballot(want < base + end));
+            if (want < seen + total) {
+                const int l = __builtin_ctzll(__ballot(want < seen + end));
                 s = s0 + l;
-                tile = want - base - __builtin_amdgcn_readlane(end - tiles, l);
+                tile = (int)(want - seen) - __builtin_amdgcn_readlane(end - tiles, l);
                 units = __builtin_amdgcn_readlane(kept ? need : 0, l);
                 end_units = __builtin_amdgcn_readlane(need_end, l);
                 break;
             }
-            base += total;
+            seen += total;
             before = __builtin_amdgcn_readlane(need_end, 63);
         }
         if (s < 0) return;

@@ -90,6 +90,8 @@ def test_arguments_that_are_refused():
         assert attend(p, **{name: None}) == NULL, name
     for name in ("Q", "K", "V", "O", "ws"):
         assert attend(p, **{name: P + 8}) == ALIGN, name
+    for name in ("table", "q_start", "kv_len", "lse", "weights"):
+        assert attend(p, **{name: P + 2}) == ALIGN, name
     for decay in (-0.5, 1.5, float("nan")):
         assert attend(p, decay=decay) == SHAPE
     assert attend(p, n=dhsa.dhsa_paged_workspace_bytes(p, False) - 1) == WORKSPACE
@@ -102,7 +104,9 @@ def test_arguments_that_are_refused():
         assert evict(p, **{name: None}) == NULL, name
     for name in ("K", "V", "ws"):
         assert evict(p, **{name: P + 8}) == ALIGN, name
-    for keep, first, recent in ((0, 0, 0), (-1, 0, 0), (4, -1, 0), (4, 0, -1), (4, 3, 2), (1 << 30, (1 << 31) - 1, (1 << 31) - 1)):
+    for name in ("table", "kv_len", "out", "kv_out", "W"):
+        assert evict(p, **{name: P + 1}) == ALIGN, name
+    for keep, first, recent in (((1 << 30) + 1, 0, 0), (0, 0, 0), (-1, 0, 0), (4, -1, 0), (4, 0, -1), (4, 3, 2), (1 << 30, (1 << 31) - 1, (1 << 31) - 1)):
         assert evict(p, keep=keep, first=first, recent=recent) == BUDGET, (keep, first, recent)
     assert evict(p, n=dhsa.dhsa_paged_evict_workspace_bytes(p, 32) - 1) == WORKSPACE
     assert dhsa.dhsa_paged_evict_workspace_bytes(p, 0) == 0
