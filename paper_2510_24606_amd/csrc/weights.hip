@@ -144,11 +144,17 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const Spa
                     s_ = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], *reinterpret_cast<const bf16x8 *>(qp + 16 * ((2 * s + g2) ^ q_sw)), s_, 0, 0, 0);
                 const float ref = sm.norm[buf][0][rb * 32 + lr], inv = R + rb * 32 + lr < R1 ? sm.norm[buf][1][rb * 32 + lr] : 0.f;
                 if (masked) {
-                    const int p = base + token_of(a, R + rb * 32 + lr < R1 ? R + rb * 32 + lr : R1 - 1);
+                    // distance to the wave's first key of this lane; one comparison says both "not behind the row" and "in the window"
+                    const int p = base + token_of(a, R + rb * 32 + lr < R1 ? R + rb * 32 + lr : R1 - 1), d = p - kw - 4 * g2;
+                    if (kw < a.sinks) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const int j = kw + (x & 3) + 8 * (x >> 2) + 4 * g2;
-                        s_[x] = j <= p && p < key_hi(a, j) ? s_[x] : -INFINITY;
+                        for (int x = 0; x < 16; ++x) {
+                            const int k = (x & 3) + 8 * (x >> 2);
+                            s_[x] = (unsigned)(d - k) < (unsigned)a.window || (kw + 4 * g2 + k < a.sinks && d >= k) ? s_[x] : -INFINITY;
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) s_[x] = (unsigned)(d - (x & 3) - 8 * (x >> 2)) < (unsigned)a.window ? s_[x] : -INFINITY;
                     }
                 }
 #pragma unroll
