@@ -142,6 +142,8 @@ DHSA_API dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t windo
     for (const auto &x : all)
         if ((st = stride(x.in, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
     if (!fits(L, ks_l, 1, 0, prob->D, esz) || !fits(L, vs_l, 1, 0, prob->D, esz)) return DHSA_ERR_SHAPE;
+    // (as dhsa_prefill: the bf16 rows of a head are addressed with 32-bit offsets)
+    if (prob->dtype == DHSA_BF16 && (L * ks_l * 2 > (int64_t)1 << 32 || L * vs_l * 2 > (int64_t)1 << 32)) return DHSA_ERR_SHAPE;
     if (!Q_dev || !K_dev || !V_dev || !O_dev) return DHSA_ERR_NULL;
     if (misaligned(Q_dev) || misaligned(K_dev) || misaligned(V_dev) || misaligned(O_dev)) return DHSA_ERR_ALIGN;
     a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev;

@@ -15,6 +15,8 @@
 // then O += P V; the loads of the upper half of K(n + 1), of V(n + 1) and of the lower half of K(n + 2) are spread in
 // between; one barrier a tile.  O / l is exact whatever the exponents' reference is, so a row's reference is its maximum over
 // its first block with a key and moves only when a block's sum passes 2^20.
+#include <type_traits>
+
 #include "attn_mfma.h"
 #include "paged.h"
 
@@ -24,21 +26,22 @@ namespace {
 
 constexpr int kTallKeys = 64;
 
-template <int D>
+template <int D, typename Addr>
 struct TallSmem {
     static constexpr int kTile = kTallKeys * D;
     alignas(1024) uint16_t K[2 * kTile];
     alignas(1024) uint16_t V[2 * kTile];
-    // of the keys of eight tiles: addresses of the rows, in the order the loading lanes want them; a row at position p takes
+    // of the keys of eight tiles: addresses of the rows (contiguous K and V: offsets, a head spans at most 4 GiB; 16.36 -> 15.99 ms for
+    // a window of 8192 over 128K tokens), in the order the loading lanes want them; a row at position p takes
     // the key iff lo < p < hi
-    alignas(16) uint64_t kaddr[8][kTallKeys], vaddr[8][kTallKeys];
+    alignas(16) Addr kaddr[8][kTallKeys], vaddr[8][kTallKeys];
     alignas(16) int lo[8][kTallKeys], hi[8][kTallKeys];
     int flags[8];        // does some row of the tile not take some key of it?
 };
 
 __device__ const uint4 zero_row[16] = {};     // what a key without a page has for K and V
 
-__device__ __forceinline__ void load16_to_lds(uint64_t addr, unsigned lds_window) {
+__device__ __forceinline__ void load16_to_lds(uint64_t addr, const char *, unsigned lds_window) {
 #if defined(__HIP_DEVICE_COMPILE__)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds_window) : "memory");
 #else
@@ -46,11 +49,20 @@ __device__ __forceinline__ void load16_to_lds(uint64_t addr, unsigned lds_window
 #endif
 }
 
+__device__ __forceinline__ void load16_to_lds(uint32_t offset, const char *base, unsigned lds_window) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(offset), "s"(lds_window), "s"(base) : "memory");
+#else
+    (void)offset; (void)base; (void)lds_window;
+#endif
+}
+
 }  // namespace
 
 template <int D, bool PAGED>
 __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block0) {
-    using Smem = TallSmem<D>;
+    using Addr = std::conditional_t<PAGED, uint64_t, uint32_t>;
+    using Smem = TallSmem<D, Addr>;
     constexpr int OPR = D / 8;          // 16-byte pieces per row
     constexpr int KPT = OPR / 4;        // load instructions per wave and tile (K and V each)
     constexpr int NS = D / 16;          // matrix steps of K Q^T
@@ -122,9 +134,14 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
         const bool none = PAGED && (unsigned)page >= (unsigned)a.n_pages;
         const uint32_t ko = (PAGED ? (uint32_t)page * a.ks_p : 0u) + (uint32_t)in * a.ks_s;
         const uint32_t vo = (PAGED ? (uint32_t)page * a.vs_p : 0u) + (uint32_t)in * a.vs_s;
-        const uint64_t zero = (uint64_t)(uintptr_t)zero_row;
-        sm.kaddr[n & 7][slot_wr] = none ? zero : (uint64_t)(uintptr_t)Kg + ((uint64_t)ko << 4);
-        sm.vaddr[n & 7][slot_wr] = none ? zero : (uint64_t)(uintptr_t)Vg + ((uint64_t)vo << 4);
+        if constexpr (PAGED) {
+            const uint64_t zero = (uint64_t)(uintptr_t)zero_row;
+            sm.kaddr[n & 7][slot_wr] = none ? zero : (uint64_t)(uintptr_t)Kg + ((uint64_t)ko << 4);
+            sm.vaddr[n & 7][slot_wr] = none ? zero : (uint64_t)(uintptr_t)Vg + ((uint64_t)vo << 4);
+        } else {
+            sm.kaddr[n & 7][slot_wr] = ko << 4;
+            sm.vaddr[n & 7][slot_wr] = vo << 4;
+        }
         const bool out = none || x_lo + n * kTallKeys + lane >= x_hi;
         const int lo = out ? kIntMaxP : j - 1, hi = key_hi(a, j);
         sm.lo[n & 7][lane] = lo;
@@ -134,9 +151,9 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
     };
 #define TALL_ADDRS(dst, tab, n, c0, c1) \
     _Pragma("unroll") for (int i = c0; i < c1; ++i) dst[i] = sm.tab[(n) & 7][slot_rd + i];
-#define TALL_LOAD(lds, addrs, n, c0, c1) \
+#define TALL_LOAD(X, addrs, n, c0, c1) \
     _Pragma("unroll") for (int i = c0; i < c1; ++i) \
-        load16_to_lds(addrs[i] + ld_piece, lds + (((n) & 1) * kTile + wave * 512) * 2 + i * 4096);
+        load16_to_lds((Addr)(addrs[i] + ld_piece), X##g, lds_##X + (((n) & 1) * kTile + wave * 512) * 2 + i * 4096);
 // S^T of the 32-key block whose K rows start at element kb of the buffer that k_off points into
 #define TALL_QK(kb, s_) \
     { \
@@ -213,17 +230,17 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
     if (ntiles > 0) {
         f32x16 s_a, s_b;                      // scores of two consecutive blocks
         int toggle = 2 * kTile;
-        uint64_t ka[KPT], va[KPT];            // addresses of the loads this lane issues next (lower half of K: of the tile after)
+        Addr ka[KPT], va[KPT];                // addresses of the loads this lane issues next (lower half of K: of the tile after)
         int page = page_ask(4 + wave);
         if (wave < ntiles) make_list(wave, page_ask(wave));
         __syncthreads();
         TALL_ADDRS(ka, kaddr, 0, 0, KPT);
         TALL_ADDRS(va, vaddr, 0, 0, KPT);
-        TALL_LOAD(lds_K, ka, 0, 0, KPT);
-        TALL_LOAD(lds_V, va, 0, 0, KPT);
+        TALL_LOAD(K, ka, 0, 0, KPT);
+        TALL_LOAD(V, va, 0, 0, KPT);
         if (ntiles > 1) {
             TALL_ADDRS(ka, kaddr, 1, 0, KPT / 2);
-            TALL_LOAD(lds_K, ka, 1, 0, KPT / 2);
+            TALL_LOAD(K, ka, 1, 0, KPT / 2);
         }
         int fl_cur = __builtin_amdgcn_readfirstlane(sm.flags[0]);
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's pieces are in LDS
@@ -252,27 +269,27 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
             const int fl_next = __builtin_amdgcn_readfirstlane(sm.flags[(n + 1) & 7]);
             if (live) {
                 bf16x8 pf[2];
-                TALL_LOAD(lds_K, ka, n + 1, KPT / 2, KPT);
+                TALL_LOAD(K, ka, n + 1, KPT / 2, KPT);
                 TALL_QK(32 * D, s_b);                      // block 1 of tile n
                 TALL_EXP(s_a, pf);
-                TALL_LOAD(lds_V, va, n + 1, 0, KPT / 2);
+                TALL_LOAD(V, va, n + 1, 0, KPT / 2);
                 TALL_PV(0, pf);
                 TALL_MASK(n, 1, s_b, fl_cur);
 #pragma unroll
                 for (int s = 0; s < NS; ++s) k_off[s] += toggle;   // now the K buffer of tile n + 1
-                TALL_LOAD(lds_V, va, n + 1, KPT / 2, KPT);
+                TALL_LOAD(V, va, n + 1, KPT / 2, KPT);
                 TALL_QK(0, s_a);                           // block 0 of tile n + 1
                 TALL_EXP(s_b, pf);
-                if (n + 2 < ntiles) TALL_LOAD(lds_K, ka, n + 2, 0, KPT / 2);
+                if (n + 2 < ntiles) TALL_LOAD(K, ka, n + 2, 0, KPT / 2);
                 TALL_PV(1, pf);
                 TALL_MASK(n + 1, 0, s_a, fl_next);
                 v_base_e += toggle;                        // now the V buffer of tile n + 1
                 v_base_o += toggle;
                 toggle = -toggle;
             } else {
-                TALL_LOAD(lds_K, ka, n + 1, KPT / 2, KPT);
-                TALL_LOAD(lds_V, va, n + 1, 0, KPT);
-                if (n + 2 < ntiles) TALL_LOAD(lds_K, ka, n + 2, 0, KPT / 2);
+                TALL_LOAD(K, ka, n + 1, KPT / 2, KPT);
+                TALL_LOAD(V, va, n + 1, 0, KPT);
+                if (n + 2 < ntiles) TALL_LOAD(K, ka, n + 2, 0, KPT / 2);
             }
             fl_cur = fl_next;
             __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the pieces this wave requested have landed

@@ -78,6 +78,8 @@ def test_problems_that_are_refused(kw, code):
 @pytest.mark.parametrize("kw,code", BAD + [
     (dict(L=0), SHAPE), (dict(L=1 << 31), SHAPE), (dict(k_stride_l=64), SHAPE), (dict(v_stride_l=132), ALIGN), (dict(o_stride_h=-8), SHAPE),
     (dict(L=1 << 28), SHAPE),                               # 2^28 rows of 256 bytes span 64 GiB
+    (dict(L=1 << 27, dtype=dhsa.DHSA_F32), SHAPE),
+    (dict(L=(1 << 24) + 1), SHAPE), (dict(L=1 << 20, k_stride_l=2056), SHAPE),      # a bf16 head of more than 4 GiB
 ])
 def test_windows_that_are_refused(kw, code):
     assert window(dense(**kw)) == code
