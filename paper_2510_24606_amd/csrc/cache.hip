@@ -7,7 +7,8 @@ namespace dhsa {
 
 // ---------------------------------------------------------------------------
 // Append: a workgroup per new token moves its rows of all kv-heads, 16 bytes a thread.  Bound by a chain of three loads (the
-// sequence of the token, its length, the page) where tokens are few, by the copy where they are many.
+// sequence of the token, its length, the page) where tokens are few (64 tokens of 8 kv-heads of 128, bf16: 3.0 us of kernel), by the
+// copy where they are many (24K tokens, 195 MB: 38.6 us, 5.1 TB/s).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_append(SpanArgs a, AppendArgs ap, int row16, int t0) {
     const int t = t0 + blockIdx.x, lane = threadIdx.x & 63;
@@ -44,7 +45,8 @@ hipError_t launch_append(const SpanArgs &a, const AppendArgs &ap, int row_bytes,
 // ---------------------------------------------------------------------------
 // Eviction, first launch: which slots stay.  A workgroup per sequence and kv-head.  The middle slots [first, kv - recent) are
 // ordered by a 32-bit key of their weight; the key of the last one that stays is found digit by digit (counts in LDS), then
-// the slots above it, and of those equal to it the first ones, are listed in order.
+// the slots above it, and of those equal to it the first ones, are listed in order.  What bounds it is the instructions of one CU
+// per list: 1.5 us for each 1024 slots, behind 7 us of passes and barriers (8 x 8 lists of 8192..32768 slots 51 us).
 // ---------------------------------------------------------------------------
 // larger weight, larger key; -0 = 0; NaN and slots without a page: 0, less than any number
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -157,7 +159,8 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
 // ---------------------------------------------------------------------------
 // Eviction, second launch: the rows move.  In place one workgroup does its columns of a head: kept slots ascend, so row t moves
 // from a slot >= t; batches are read whole before they are written, and a batch is written below everything that a later one
-// reads.  Into other pages every batch has a workgroup of its own (8 x 8 heads, 4096 rows each: 100 us with one for all).
+// reads.  Into other pages every batch has a workgroup of its own: 8 x 8 heads, 4096 rows each of K and V, 268 MB read and written,
+// 66 us (4.1 TB/s; 100 us with one workgroup for all batches).
 // blockIdx.x: part (K columns, V columns, weights) and batch, y: kv-head, z: sequence.
 // ---------------------------------------------------------------------------
 constexpr int kMoveU = 4;

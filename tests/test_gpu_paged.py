@@ -158,6 +158,22 @@ def test_many_sequences(n_seq):
     run(lens, 4, 2, 64, BF16, 16, weights=True)
 
 
+@pytest.mark.parametrize("dtype,D", [(F32, 64), (F32, 128), (BF16, 64), (BF16, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 3)])
+def test_few_rows_in_the_mean(window, sinks, dtype, D):
+    """Small tiles, several of them a sequence: scores of 24 rows are kept, those of 80 are made again for the weights."""
+    run([(1, 50)] * 9 + [(6, 500)] + [(1, 33)] * 3, 8, 2, D, dtype, 16, weights=True, window=window, sinks=sinks)
+    run([(1, 40)] * 30 + [(20, 300), (2, 31)], 8, 2, D, dtype, 24, weights=True, decay=0.5, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scores_that_do_not_fit(dtype):
+    """The workspace keeps scores for as many rows as a sequence has in the mean: of one with eight times as many, and of those
+    behind it, they are made again."""
+    run([(1, 16)] * 5 + [(8, 2000)] + [(1, 16)] * 25, 8, 2, 64, dtype, 16, weights=True)
+    run([(8, 2000)] + [(1, 16)] * 30, 4, 1, 128, dtype, 64, weights=True, window=300, sinks=70)
+
+
 def test_long_and_short_together():
     """One conversation is cut into many pieces beside short ones; sums over 40000 keys."""
     run([(1, 9), (1, 40000), (2, 70), (0, 10), (1, 1000)], 4, 1, 128, BF16, 64, weights=True)

@@ -63,6 +63,15 @@ def test_long_prompts(L, H_q, H_kv, window, sinks, dtype):
     check(L, H_q, H_kv, 128 if dtype == BF16 else 64, dtype, window, sinks, rows=rows)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("L,window,sinks", [(1300, 200, 3), (1700, 1700, 0), (2100, 77, 100), (2400, 500, 1)])
+def test_prompts_of_every_tile_height(L, window, sinks, dtype):
+    """8 heads of 2 kv-heads: tiles of 16, 32 and 128 rows as the prompt gets longer."""
+    rows = torch.unique(torch.cat([torch.arange(20), torch.arange(L - 140, L), torch.randint(0, L, (100,), generator=torch.Generator().manual_seed(L))]))
+    for D in (64, 128):
+        check(L, 8, 2, D, dtype, window, sinks, "lhd", rows=rows)
+
+
 def test_scale_and_large_scores():
     check(200, 4, 2, 64, BF16, 90, 2, scale=3.0)        # scores around 200: one key has nearly all of a row
     check(200, 4, 2, 128, F32, 90, 2, scale=0.01)
