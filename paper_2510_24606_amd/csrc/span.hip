@@ -399,9 +399,10 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
     __shared__ float s_m[16], s_l[16], s_o[16][D];
     const int tid = threadIdx.x, lane = tid & 63, grp = tid >> 4, c0 = (tid & 15) * CPL;
     const int64_t rows = a.T * a.H_kv * a.G, r0 = (int64_t)blockIdx.x * per;
-    const int end = a.q_start[a.n_seq];          // rows from there on are nobody's: what lies in `cut` means nothing
+    const int begin = a.q_start[0], end = a.q_start[a.n_seq];      // other rows are nobody's: what lies in `cut` means nothing
     int2 cut = make_int2(0, 0);
-    if (lane < per && r0 + lane < rows && (int)((r0 + lane) % a.T) < end) cut = a.cut[r0 + lane];
+    const int t_me = (int)((r0 + lane) % a.T);
+    if (lane < per && r0 + lane < rows && t_me >= begin && t_me < end) cut = a.cut[r0 + lane];
     // (nor where the arrays are no sequences: nothing is read outside the states)
     const bool is_cut = cut.y > 1 && cut.x >= 0 && cut.x / a.M + (int64_t)(cut.y - 1) * a.H_kv < a.part_cap;
     for (unsigned long long left = __ballot(is_cut); left; left &= left - 1) {

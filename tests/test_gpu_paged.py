@@ -239,6 +239,26 @@ def test_lengths_that_do_not_fit():
     assert (b.K[page, :, :3] == 0).all() and not (b.K[page, :, 3:] == 0).all()
 
 
+def test_rows_that_are_nobodys():
+    """Rows before the first sequence and behind the last one stay as they were, also where others are cut into pieces and the
+    workspace holds what an earlier call left."""
+    b = Batch([(2, 3000), (1, 40)], 4, 2, 64, BF16, 16, extra_rows=2)
+    ws = dhsa.alloc_paged(b.prob)
+    O, lse = b.attend(ws=ws)
+    b.check(O, lse)
+    dhsa.dhsa_paged_attend(b.prob, b.Q, b.K, b.V, b.table, b.q_start, b.kv_len, O, ws, lse=lse)      # leaves its states in ws
+    b.q_start = torch.tensor([1, 2, 3], dtype=torch.int32).cuda()
+    O2, lse2 = torch.full_like(b.Q, 7.0), torch.full((4, b.T), 7.0, device="cuda")
+    dhsa.dhsa_paged_attend(b.prob, b.Q, b.K, b.V, b.table, b.q_start, b.kv_len, O2, ws, lse=lse2)
+    torch.cuda.synchronize()
+    for x in (O2, lse2):
+        assert (x[:, :1] == 7.0).all() and (x[:, 3:] == 7.0).all() and not (x[:, 1:3] == 7.0).all()
+    for g in range(2):
+        o, z, _, t_o, t_z, _ = paged_plain.attend(b.Q[2 * g:2 * g + 2, 1:2].cpu(), b.kc[0][g], b.vc[0][g], torch.tensor([2999]), 0, 0)
+        paged_plain.close(O2[2 * g:2 * g + 2, 1:2], o, t_o, "O")
+        paged_plain.close(lse2[2 * g:2 * g + 2, 1:2], z, t_z, "lse")
+
+
 def test_a_pool_beyond_32_bits():
     """Pages whose offsets pass 2^32 bytes and 2^31 elements."""
     page, H_kv, D = 64, 2, 128
@@ -586,6 +606,39 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for x, y in zip(got, (O, lse, a.K, a.V, W, kv_out, idx)):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured calls of different lengths over one workspace, replayed in turn, eager calls in between."""
+    a, b = Batch([(1, 3000), (1, 50)], 4, 2, 64, BF16, 16, seed=1), Batch([(1, 20), (1, 4000)], 4, 2, 64, BF16, 16, seed=2)
+    ws = torch.empty(max(dhsa.dhsa_paged_workspace_bytes(x.prob) for x in (a, b)), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for x in (a, b):
+        O, lse, W = torch.empty_like(x.Q), torch.empty((4, x.T), device="cuda"), x.new_weights()
+        before = W.clone()
+
+        def call(x=x, O=O, lse=lse, W=W):
+            dhsa.dhsa_paged_attend(x.prob, x.Q, x.K, x.V, x.table, x.q_start, x.kv_len, O, ws, lse=lse, weights=W, decay=0.0)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append((x, O, lse, W, before, graph, call))
+    for turn in range(3):
+        for x, O, lse, W, before, graph, call in graphs:
+            for y in (O, lse):
+                y.fill_(7.0)
+            graph.replay()
+            if turn == 1:
+                call()
+        torch.cuda.synchronize()
+        for x, O, lse, W, before, graph, call in graphs:
+            x.check(O, lse, before, W, 0.0)
 
 
 def test_refusals_on_the_device():
