@@ -182,28 +182,32 @@ __device__ __forceinline__ void move_rows(const SpanArgs &a, const EvictArgs &e,
     // lanes threads per row, width bytes each; strides in `unit` bytes
     const int tid = threadIdx.x, r = tid / lanes, c = tid % lanes * width, rows = THREADS / lanes;
     const int32_t *table = a.table + (int64_t)s * a.max_pages, *table_out = e.table_out + (int64_t)s * a.max_pages;
-    const auto place = [&](const int32_t *tb, int slot) -> char * {
-        const int pi = page_of(a, slot), page = tb[pi];
-        if ((unsigned)page >= (unsigned)a.n_pages) return nullptr;
-        return base + ((uint64_t)page * p16 + (uint64_t)(slot - pi * a.page_size) * s16) * unit + c;
+    const auto place = [&](int page, int slot) {
+        return base + ((uint64_t)page * p16 + (uint64_t)(slot - page_of(a, slot) * a.page_size) * s16) * unit + c;
     };
     for (int t0 = batch * rows * kMoveU; t0 < n; t0 += batches * rows * kMoveU) {
+        // slots, pages, rows: each of the kMoveU is asked for beside the others
         V x[kMoveU];
-        char *to[kMoveU];
+        int to[kMoveU], from[kMoveU], from_page[kMoveU], to_page[kMoveU];
+        bool ok[kMoveU];
 #pragma unroll
         for (int u = 0; u < kMoveU; ++u) {
-            const int t = t0 + u * rows + r;
-            to[u] = nullptr;
+            to[u] = t0 + u * rows + r < n ? t0 + u * rows + r : n - 1;
+            from[u] = list[to[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u) { from_page[u] = table[page_of(a, from[u])]; to_page[u] = table_out[page_of(a, to[u])]; }
+#pragma unroll
+        for (int u = 0; u < kMoveU; ++u) {
+            const bool stays = table == table_out && from[u] == to[u];
+            ok[u] = t0 + u * rows + r < n && !stays && (unsigned)from_page[u] < (unsigned)a.n_pages && (unsigned)to_page[u] < (unsigned)a.n_pages;
             x[u] = V{};
-            if (t < n && !(table == table_out && list[t] == t)) {
-                const char *from = place(table, list[t]);
-                if (from) { x[u] = *reinterpret_cast<const V *>(from); to[u] = place(table_out, t); }
-            }
+            if (ok[u]) x[u] = *reinterpret_cast<const V *>(place(from_page[u], from[u]));
         }
         if constexpr (THREADS == kEvictThreads) __syncthreads();
 #pragma unroll
         for (int u = 0; u < kMoveU; ++u)
-            if (to[u]) *reinterpret_cast<V *>(to[u]) = x[u];
+            if (ok[u]) *reinterpret_cast<V *>(place(to_page[u], to[u])) = x[u];
         if constexpr (THREADS == kEvictThreads) __syncthreads();
     }
 }
