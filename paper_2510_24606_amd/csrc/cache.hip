@@ -46,7 +46,7 @@ hipError_t launch_append(const SpanArgs &a, const AppendArgs &ap, int row_bytes,
 // Eviction, first launch: which slots stay.  A workgroup per sequence and kv-head.  The middle slots [first, kv - recent) are
 // ordered by a 32-bit key of their weight; the key of the last one that stays is found digit by digit (counts in LDS), then
 // the slots above it, and of those equal to it the first ones, are listed in order.  What bounds it is the instructions of one CU
-// per list: 1.5 us for each 1024 slots, behind 7 us of passes and barriers (8 x 8 lists of 8192..32768 slots 51 us).
+// per list: 1 us for each 1024 slots, behind 7 us of passes and barriers (8 x 8 lists of 8192..32768 slots 40 us).
 // ---------------------------------------------------------------------------
 // larger weight, larger key; -0 = 0; NaN and slots without a page: 0, less than any number
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
     if (need == 0) return;
     const int32_t *table = a.table + (int64_t)s * a.max_pages;
     const int rounds = (m1 - m0 + kEvictThreads - 1) / kEvictThreads, w0 = m0 + wave * rounds * 64;
-    // (page numbers and weights are asked for in two batches, without a branch between them: one by one each round of the wave took
+    // (page numbers and weights are asked for eight at a time, without a branch between them: one by one each round of the wave took
     // two trips to memory, 51 us for the lists above)
     const auto page_at = [&](int slot) { return table[page_of(a, slot)]; };
     const auto weight_at = [&](int slot, int page) {
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
 // Eviction, second launch: the rows move.  In place one workgroup does its columns of a head: kept slots ascend, so row t moves
 // from a slot >= t; batches are read whole before they are written, and a batch is written below everything that a later one
 // reads.  Into other pages every batch has a workgroup of its own: 8 x 8 heads, 4096 rows each of K and V, 268 MB read and written,
-// 66 us (4.1 TB/s; 100 us with one workgroup for all batches).
+// 50 us (5.3 TB/s; 100 us with one workgroup for all batches).
 // blockIdx.x: part (K columns, V columns, weights) and batch, y: kv-head, z: sequence.
 // ---------------------------------------------------------------------------
 constexpr int kMoveU = 4;
