@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
         __builtin_amdgcn_wave_barrier();
     };
     // Scores that are kept gather in LDS, as many blocks as kFewRows allows, before they are stored: the rows of later keys come behind
-    // a store that was issued before them (64 conversations: 413 us without scores, 497 when every block stored its own).
+    // a store that was issued before them (64 conversations, one block at a time: 515 us so, 535 when every block stored its own).
     // (There is room for whole blocks in memory, and pieces begin at multiples of 4 BK.)
     int kept = 0;
     const int keep_most = PAGED && it.scores ? kFewRows / it.rows : 0, keep_step = keep_most > 0 ? it.q.n * a.G * 32 : 0;   // floats from block of 32 keys to block
