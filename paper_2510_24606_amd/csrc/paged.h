@@ -38,6 +38,12 @@ struct SpanArgs {
     int score_units;
 };
 
+// What a row's state (reference m, log2; sum l) gives.  Without a key m = -inf and l = 0; a row whose scores are NaN has l = NaN and
+// says so in O and lse, while a key that it does not see has its factor of 0 in the weights (those that it sees have its NaN score).
+__device__ __forceinline__ float inv_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
+__device__ __forceinline__ float2 norm_of(float m, float l) { return l > 0.f ? make_float2(m, 1.f / l) : make_float2(1e30f, 0.f); }
+
 constexpr int kIntMaxP = 0x7fffffff;
 constexpr int kFewRows = 32;
 constexpr int kScoreUnitsMax = 1 << 24;      // 4 GiB; 64 times that fits 32 bits

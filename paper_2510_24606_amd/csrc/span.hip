@@ -375,13 +375,13 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
             if (c0 == 0) a.state[(int64_t)it.slot * M + row] = make_float2(mx, l);
             continue;
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;         // no visible key: zeros
+        const float inv = inv_of(l);                       // no visible key: zeros
         T *op = (T *)a.O + h * a.os_h + t * a.os_t + c0;
 #pragma unroll
         for (int e = 0; e < CPL; ++e) store_out(op + e, o[e] * inv);
         if (c0 == 0) {
-            if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
-            if (a.norm) a.norm[h * a.T + t] = make_float2(l > 0.f ? mx : 1e30f, inv);
+            if (a.lse) a.lse[h * a.T + t] = lse_of(mx, l);
+            if (a.norm) a.norm[h * a.T + t] = norm_of(mx, l);
         }
     }
 }
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (x0 + 16 * u >= pieces || st[u].x == -INFINITY) continue;
+                if (x0 + 16 * u >= pieces || st[u].y == 0.f) continue;      // no key there
                 const float m_new = fmaxf(mx, st[u].x);
                 const float f0 = __builtin_amdgcn_exp2f(mx - m_new), f1 = __builtin_amdgcn_exp2f(st[u].x - m_new);
                 l = l * f0 + st[u].y * f1;
@@ -452,11 +452,10 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
             const int64_t r = r0 + i;
             const int h = (int)(r / a.T);
             const int64_t t = r - h * a.T;
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
-            store_out((T *)a.O + h * a.os_h + t * a.os_t + tid, acc * inv);
+            store_out((T *)a.O + h * a.os_h + t * a.os_t + tid, acc * inv_of(sum));
             if (tid == 0) {
-                if (a.lse) a.lse[r] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
-                if (a.norm) a.norm[r] = make_float2(sum > 0.f ? m : 1e30f, inv);
+                if (a.lse) a.lse[r] = lse_of(m, sum);
+                if (a.norm) a.norm[r] = norm_of(m, sum);
             }
         }
     }

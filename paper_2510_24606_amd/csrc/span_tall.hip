@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
         if (g2 == 0) a.state[at] = make_float2(mx, l);
         return;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;   // no visible key: zeros
+    const float inv = inv_of(l);                 // no visible key: zeros
     uint16_t *op = (uint16_t *)a.O + h * a.os_h + t * a.os_t;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -347,8 +347,8 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
             *reinterpret_cast<uint2 *>(op + db * 32 + q4 * 8 + g2 * 4) = pk.u;
         }
     if (g2 == 0) {
-        if (a.lse) a.lse[h * a.T + t] = l > 0.f ? (mx + log2f(l)) * 0.69314718055994531f : -INFINITY;
-        if (a.norm) a.norm[h * a.T + t] = make_float2(l > 0.f ? mx : 1e30f, inv);
+        if (a.lse) a.lse[h * a.T + t] = lse_of(mx, l);
+        if (a.norm) a.norm[h * a.T + t] = norm_of(mx, l);
     }
 }
 

@@ -1,0 +1,61 @@
+"""The paged cache at what its callers may hand over by mistake or in passing."""
+import pytest
+import torch
+
+import paged_plain
+import paper_2510_24606_amd as dhsa
+from test_gpu_paged import Batch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 64), (F32, 128), (BF16, 64), (BF16, 128)])
+@pytest.mark.parametrize("lens,row", [([(1, 40), (1, 30)], 0), ([(1, 9000), (1, 20)], 0), ([(1, 20), (3, 9000)], 2),
+                                      ([(70, 90), (3, 40)], 33), ([(60, 9000), (2, 50)], 7), ([(200, 300)], 199)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 3)])
+def test_a_row_that_is_not_a_number(lens, row, window, sinks, dtype, D):
+    """It says so in O, in lse and in the weights of the keys that it sees, however long the cache is; nothing else does."""
+    b = Batch(lens, 4, 2, D, dtype, 16, window=window, sinks=sinks)
+    W, W2 = b.new_weights(), b.new_weights()
+    before = W.clone()
+    O, lse = b.attend(W, 0.0)
+    Q = b.Q.clone()
+    b.Q[1, row, D // 2] = float("nan")                  # one head of the first kv-head
+    O2, lse2 = b.attend(W2, 0.0)
+    assert torch.isnan(O2[1, row]).all() and torch.isnan(lse2[1, row])
+    for s, (n, kv) in enumerate(lens):
+        page, slot = (x.cuda() for x in b.slots(s))
+        sees = torch.zeros(kv, dtype=torch.bool)
+        if b.starts[s] <= row < b.starts[s + 1]:
+            sees = paged_plain.sees(torch.tensor([kv - n + row - b.starts[s]]), kv, window, sinks)[0]
+        got = W2[page, :, slot]
+        assert torch.equal(torch.isnan(got[:, 0]).cpu(), sees) and not torch.isnan(got[:, 1]).any()
+        W[page, :, slot] = torch.where(torch.isnan(got), W[page, :, slot], got)
+    b.Q, O2[1, row], lse2[1, row] = Q, O[1, row], lse[1, row]
+    b.check(O2, lse2, before, W, 0.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("L", [50, 700, 5000])
+def test_a_row_of_a_prompt_that_is_not_a_number(L, dtype):
+    g = torch.Generator().manual_seed(L)
+    Q, K, V = (torch.randn((h, L, 64), generator=g).to(dtype).cuda() for h in (8, 2, 2))
+    O, O2 = torch.empty_like(Q), torch.empty_like(Q)
+    p = dhsa.problem(Q, K, [0, L], L)
+    dhsa.dhsa_window_prefill(p, Q, K, V, O, 100, 2)
+    Q[3, L // 2, 5] = float("nan")
+    dhsa.dhsa_window_prefill(p, Q, K, V, O2, 100, 2)
+    torch.cuda.synchronize()
+    assert torch.isnan(O2[3, L // 2]).all()
+    O2[3, L // 2] = O[3, L // 2]
+    rows = torch.unique(torch.cat([torch.arange(max(0, L // 2 - 140), min(L, L // 2 + 140)), torch.arange(20)]))
+    for h in range(2):
+        q = Q[4 * h:4 * h + 4, rows.cuda()].nan_to_num(0.0).cpu()
+        o, _, _, tol, _, _ = paged_plain.attend(q, K[h].cpu(), V[h].cpu(), rows, 100, 2)
+        got = O2[4 * h:4 * h + 4, rows.cuda()].cpu()
+        if h == 0:
+            at = int((rows == L // 2).nonzero())
+            got[3, at] = o[3, at].to(dtype)
+        paged_plain.close(got, o, tol, f"kv-head {h}")
