@@ -374,10 +374,11 @@ dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t window, int64_
  *          (0 or more), in the slots kv_len[s] - n_s .. kv_len[s] - 1.  Not descending, from 0.
  * These arrays are read by the kernels when the call runs: a captured graph may be replayed
  * with other lengths and pages in them, as long as n_seq and T bound what is there.  They
- * are not validated on the host; what the kernels find is clamped: rows behind T and slots
- * behind max_pages page_size are not touched, a page outside [0, n_pages) is never read or
- * written (its keys are left out), a row with more new tokens before it than kv_len allows
- * sees no key.  Rows of Q behind q_start[n_seq] are not read, theirs of O left as they were.
+ * are not validated on the host; the kernels leave out what does not fit: rows behind T and
+ * slots behind max_pages page_size are not touched (a new token whose slot lies there is not
+ * appended, its row attends to the slots before it that there are), a page outside [0, n_pages)
+ * is never read or written (its keys are left out), a row with more new tokens before it than
+ * kv_len allows sees no key.  Rows and slots that are there keep their places.  Rows of Q behind q_start[n_seq] are not read, theirs of O left as they were.
  * The rows of slots [0, kv_len) must be finite (pages behind that are never read).
  * Sequences may share pages that are only read; a page that a call writes (append, evict,
  * weights) must be in one place of one sequence's table.

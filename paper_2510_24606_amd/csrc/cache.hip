@@ -16,8 +16,8 @@ __global__ __launch_bounds__(256) void k_append(SpanArgs a, AppendArgs ap, int r
     for (int s0 = 0; s0 < a.n_seq; s0 += 64) s += __popcll(__ballot(s0 + lane < a.n_seq && a.q_start[s0 + lane + 1] <= t));
     if (s >= a.n_seq) return;
     const Seq q = read_seq(a, s);
-    const int slot = q.kv - q.n + (t - (int)q.q0);
-    if (t < q.q0 || t >= q.q0 + q.n || slot < 0) return;
+    const int slot = q.base + (t - (int)q.q0);
+    if (t < q.q0 || t >= q.q0 + q.n || slot < 0 || slot >= q.kv) return;
     const int pi = page_of(a, slot), in = slot - pi * a.page_size, page = a.table[(int64_t)s * a.max_pages + pi];
     if ((unsigned)page >= (unsigned)a.n_pages) return;
     const int64_t kd = (int64_t)((uint64_t)((uint32_t)page * a.ks_p + (uint32_t)in * a.ks_s) << 4);

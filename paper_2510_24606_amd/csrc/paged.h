@@ -48,34 +48,40 @@ constexpr int kIntMaxP = 0x7fffffff;
 constexpr int kFewRows = 32;
 constexpr int kScoreUnitsMax = 1 << 24;      // 4 GiB; 64 times that fits 32 bits
 
-// One sequence as the kernels see it: whatever is in the arrays, rows stay below T and slots below slots_max.
+// One sequence as the kernels see it: whatever is in the arrays, rows stay below T and slots below slots_max.  What does not fit is
+// left out; the rows and slots that are there keep their places.
 struct Seq {
     int64_t q0;   // first row
-    int n, kv;    // new tokens, tokens
+    int n, kv;    // rows, slots that there are
+    int base;     // slot (position) of the first row: negative for rows that see nothing, kv and more for those behind the slots
 };
 __device__ __forceinline__ Seq read_seq(const SpanArgs &a, int s) {
     Seq q;
-    if (!a.q_start) { q.q0 = 0; q.n = q.kv = (int)a.T; return q; }
+    if (!a.q_start) { q.q0 = 0; q.n = q.kv = (int)a.T; q.base = 0; return q; }
     int b = a.q_start[s], e = a.q_start[s + 1], kv = a.kv_len[s];
     const int T = (int)a.T;
     b = b < 0 ? 0 : b > T ? T : b;
+    const int64_t base = (int64_t)kv - e + b;            // the row before e has slot kv - 1
     e = e < b ? b : e > T ? T : e;
     kv = kv < 0 ? 0 : kv > a.slots_max ? a.slots_max : kv;
     q.q0 = b; q.n = e - b; q.kv = kv;
+    q.base = base < -q.n ? -q.n : q.n == 0 ? 0 : (int)base;     // (below -n: all rows see nothing, however far below)
     return q;
 }
 
-// The keys that the rows at positions p0 .. p1 (p0 <= p1) see: slots [0, sinks_in) and [lo, hi), packed one behind the other.
+// The keys of the slots [0, kv) that the rows at positions p0 .. p1 (p0 <= p1) see: [0, head) and [lo, hi), packed one behind the
+// other.
 struct Span {
     int lo, head, total;     // packed position x is slot x for x < head, x - head + lo behind
     __device__ __forceinline__ int slot(int x) const { return x < head ? x : x - head + lo; }
 };
-__device__ __forceinline__ Span make_span(const SpanArgs &a, int p0, int p1) {
+__device__ __forceinline__ Span make_span(const SpanArgs &a, int p0, int p1, int kv) {
     Span s;
+    const int hi = p1 < 0 ? 0 : p1 < kv ? p1 + 1 : kv;
     s.lo = p0 >= a.window ? p0 - a.window + 1 : 0;
+    s.lo = s.lo < hi ? s.lo : hi;
     s.head = a.sinks < s.lo ? a.sinks : s.lo;
-    const int rest = p1 + 1 - s.lo;
-    s.total = p1 < 0 ? 0 : s.head + rest;
+    s.total = s.head + hi - s.lo;
     return s;
 }
 
@@ -133,8 +139,8 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
         *q = read_seq(a, s);
         *tiles = (int)(((int64_t)q->n * a.G + M - 1) / M);
         const int t_in = (M + a.G - 1) / a.G + 1;                       // most tokens a tile touches
-        const int p1 = q->kv - 1, p0 = p1 - t_in + 1 > 0 ? p1 - t_in + 1 : 0;
-        *units = (make_span(a, p0, p1).total + U - 1) / U;
+        const int p1 = q->base + q->n - 1, p0 = p1 - t_in + 1 > 0 ? p1 - t_in + 1 : 0;
+        *units = (make_span(a, p0, p1, q->kv).total + U - 1) / U;
     };
     Seq q;
     int tiles, units;
@@ -169,7 +175,7 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
             const auto of = [l](int x) { return __builtin_amdgcn_readlane(x, l); };
             it->s = s0 + l;
             it->g = g;
-            it->q.q0 = of((int)q.q0); it->q.n = of(q.n); it->q.kv = of(q.kv);
+            it->q.q0 = of((int)q.q0); it->q.n = of(q.n); it->q.kv = of(q.kv); it->q.base = of(q.base);
             const int at = want - of(from), t = of(tiles);
             it->pieces = of(pieces);
             it->piece = at % it->pieces;

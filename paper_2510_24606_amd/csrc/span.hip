@@ -183,9 +183,9 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
     Item it;
     if (!find_item(a, block0 + blockIdx.x, M, 4 * BK, &it)) return;
     if (it.pieces > 1 && (unsigned)it.slot >= (unsigned)a.part_cap) return;      // (there are never so many)
-    const int base = it.q.kv - it.q.n;                       // position of the first new token
+    const int base = it.q.base;                              // position of the first new token
     const int p_lo = base + it.R0 / a.G, p_hi = base + (it.R0 + it.rows - 1) / a.G;
-    const Span span = make_span(a, p_lo, p_hi);
+    const Span span = make_span(a, p_lo, p_hi, it.q.kv);
     const int units = (span.total + 4 * BK - 1) / (4 * BK), per = (units + it.pieces - 1) / it.pieces;
     const int x_lo = it.piece * per * 4 * BK;
     const int x_hi = x_lo + per * 4 * BK < span.total ? x_lo + per * 4 * BK : span.total;

@@ -78,9 +78,9 @@ __global__ __launch_bounds__(256, 2) void k_span_tall(SpanArgs a, unsigned block
     if (it.pieces > 1 && (unsigned)it.slot >= (unsigned)a.part_cap) return;      // (there are never so many)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 31, g2 = lane >> 5;
-    const int base = it.q.kv - it.q.n;                       // position of the first new token
+    const int base = it.q.base;                              // position of the first new token
     const int p_lo = base + it.R0 / a.G, p_hi = base + (it.R0 + it.rows - 1) / a.G;
-    const Span span = make_span(a, p_lo, p_hi);
+    const Span span = make_span(a, p_lo, p_hi, it.q.kv);
     const int units = (span.total + kTallKeys - 1) / kTallKeys, per = (units + it.pieces - 1) / it.pieces;
     const int x_lo = it.piece * per * kTallKeys;
     const int x_hi = x_lo + per * kTallKeys < span.total ? x_lo + per * kTallKeys : span.total;

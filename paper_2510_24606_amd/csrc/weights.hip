@@ -41,12 +41,12 @@ template <int D> struct WeightsSmem<float, D> {
 
 // The rows (of a kv-head) that may see one of the keys j0 .. j1: [r0, r1)
 __device__ __forceinline__ void rows_of(const SpanArgs &a, const Seq &sq, int j0, int j1, int *r0, int *r1) {
-    const int base = sq.kv - sq.n;
-    const int t0 = j0 > base ? j0 - base : 0;
-    const int far = key_hi(a, j1);                     // no position from here on sees the last key
-    const int t1 = j0 < a.sinks || far >= sq.kv ? sq.n : far - base;
+    const int64_t first = (int64_t)j0 - sq.base;       // row of the token at j0
+    const int64_t far = (int64_t)key_hi(a, j1) - sq.base;      // no row from here on sees the last key
+    const int t0 = first < 0 ? 0 : first < sq.n ? (int)first : sq.n;
+    const int t1 = j0 < a.sinks || far >= sq.n ? sq.n : far < t0 ? t0 : (int)far;
     *r0 = t0 * a.G;
-    *r1 = t1 > t0 ? t1 * a.G : *r0;
+    *r1 = t1 * a.G;
 }
 
 __device__ __forceinline__ void put_weight(const SpanArgs &a, const int32_t *table, int g, int j, float *W, float decay, float x) {
@@ -90,7 +90,7 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<bf16_t, D> &sm, const Spa
                                            int keys) {
     constexpr int OPR = D / 8, NS = D / 16, LPS = 64 * OPR / 256, RPW = 64 / OPR;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lr = lane & 31, g2 = lane >> 5, base = sq.kv - sq.n;
+    const int lr = lane & 31, g2 = lane >> 5, base = sq.base;
     const float c = a.scale_log2e;
     int R0, R1;
     rows_of(a, sq, j0, j0 + keys - 1, &R0, &R1);
@@ -182,7 +182,7 @@ __device__ __forceinline__ void heavy_sums(WeightsSmem<float, D> &sm, const Span
                                            int keys) {
     constexpr int NT = D / 16;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15, q = lane >> 4, base = sq.kv - sq.n;
+    const int n = lane & 15, q = lane >> 4, base = sq.base;
     const float c = a.scale_log2e;
     f32x4_t kf[4][NT], sum[4];
 #pragma unroll
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
             continue;
         }
         // kept scores: row R of tile R / M has them in the order of the tile's span
-        const int rows = sq.n * a.G, base = sq.kv - sq.n;
+        const int rows = sq.n * a.G, base = sq.base;
         const float *from = a.scores + (int64_t)(end_units - units) * 64 + (int64_t)g * rows * ((sq.kv + 63) >> 6 << 6);
         constexpr int U = kKeptKeys / 1024;
         const int j0 = tile * kKeptKeys + 4 * tid;
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
         for (int R = 0; R < rows; ++R) {
             const int t = token_of(a, R), R0 = R / a.M * a.M;
             const int R_end = (R0 + a.M < rows ? R0 + a.M : rows) - 1;
-            const Span span = make_span(a, base + token_of(a, R0), base + token_of(a, R_end));
+            const Span span = make_span(a, base + token_of(a, R0), base + token_of(a, R_end), sq.kv);
             const float2 nm = a.norm[(int64_t)(g * a.G + R - t * a.G) * a.T + sq.q0 + t];
             f32x4_t x[U];
 #pragma unroll

@@ -59,3 +59,54 @@ def test_a_row_of_a_prompt_that_is_not_a_number(L, dtype):
             at = int((rows == L // 2).nonzero())
             got[3, at] = o[3, at].to(dtype)
         paged_plain.close(got, o, tol, f"kv-head {h}")
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 64), (BF16, 128)])
+def test_tokens_behind_the_table_are_left_out(dtype, D):
+    """A sequence that is said to be longer than its table: the tokens that fit go where they belong, the slots before them and the
+    weights there stay, the other tokens go nowhere."""
+    for n, kv, cap in ((10, 69, 64), (10, 64, 64), (3, 80, 64), (64, 70, 64), (100, 90, 64), (1, 65, 64), (5, (1 << 31) - 1, 64)):
+        b = Batch([(2, 20), (n, cap), (1, 7)], 4, 2, D, dtype, 16)
+        assert b.table.shape[1] * 16 == cap
+        b.K.nan_to_num_(3.0); b.V.nan_to_num_(3.0)
+        b.kv_len[1] = kv
+        Kn, Vn = (torch.randn((2, b.T, D), generator=b.g).to(dtype).cuda() for _ in range(2))
+        W = b.new_weights()
+        K, V, W2 = b.K.clone(), b.V.clone(), W.clone()
+        dhsa.dhsa_paged_append(b.prob, Kn, Vn, b.K, b.V, b.table, b.q_start, b.kv_len, W)
+        torch.cuda.synchronize()
+        table = b.table.cpu()
+        for s, (rows, end) in enumerate(((2, 20), (n, kv), (1, 7))):
+            for i in range(rows):
+                slot = end - rows + i
+                if 0 <= slot < cap:
+                    page, at = int(table[s, slot // 16]), slot % 16
+                    K[page, :, at], V[page, :, at] = Kn[:, b.starts[s] + i], Vn[:, b.starts[s] + i]
+                    W2[page, :, at] = 0.0
+        assert torch.equal(b.K, K) and torch.equal(b.V, V) and torch.equal(W, W2), (n, kv)
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 64), (BF16, 128)])
+@pytest.mark.parametrize("n,over", [(3, 2), (10, 3), (40, 25), (150, 60), (30, 40), (6, (1 << 31) - 65)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_rows_behind_the_table_keep_their_places(n, over, window, sinks, dtype, D):
+    """Rows of such tokens attend to the slots that there are, from where they are; so do rows that are said to end behind T."""
+    cap = 64
+    b = Batch([(2, 20), (n, cap)], 4, 2, D, dtype, 16, window=window, sinks=sinks)
+    b.kv_len[1] = cap + over
+    pos = cap + over - n + torch.arange(n, dtype=torch.int64)
+    for far in (0, 9):
+        if far:
+            if over > 1000:
+                continue
+            b.q_start[2] += far                        # nine more rows than there are, and as many more tokens
+            b.kv_len[1] += far
+        W = b.new_weights()
+        O, lse = b.attend(W, 0.0)
+        for g in range(2):
+            rows = slice(2, 2 + n)
+            o, z, got, t_o, t_z, t_w = paged_plain.attend(b.Q[2 * g:2 * g + 2, rows].cpu(), b.kc[1][g], b.vc[1][g], pos, window, sinks)
+            paged_plain.close(O[2 * g:2 * g + 2, rows], o, t_o, "O")
+            paged_plain.close(lse[2 * g:2 * g + 2, rows], z, t_z, "lse")
+            page, slot = b.slots(1)
+            paged_plain.close(W[page, g, slot], got, t_w, "weights")
