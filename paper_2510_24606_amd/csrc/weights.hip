@@ -321,8 +321,9 @@ __global__ __launch_bounds__(256, 2) void k_weights(SpanArgs a, float *__restric
 hipError_t launch_weights(const SpanArgs &a, int D, int dtype, float *W, float decay, hipStream_t s) {
     // One workgroup a share where the pool's slots are in one sequence each (they take further ones where they are not): shares differ
     // by how many rows see their keys, and the chip hands out workgroups as others end.  Chunks of 1..1024 tokens of 12 sequences, 1024
-    // workgroups with every 1024th share 358 us.
-    const int64_t keys = a.scores ? kKeptKeys : dtype == DHSA_F32 ? Heavy<float>::kKeys : Heavy<bf16_t>::kKeys;
+    // workgroups with every 1024th share 358 us.  Where scores may be kept shares are up to 64 times as large and there is no telling
+    // how many: at most 1024 workgroups, so that a step of a batch does not begin with tens of thousands that find nothing.
+    const int64_t keys = dtype == DHSA_F32 ? Heavy<float>::kKeys : Heavy<bf16_t>::kKeys;
     const int64_t shares = ((int64_t)a.n_pages * a.page_size / keys + a.n_seq) * a.H_kv;
     const dim3 grid((unsigned)std::min<int64_t>(shares, a.scores ? 1024 : 1 << 16));
     if (dtype == DHSA_F32) {

@@ -1,0 +1,29 @@
+"""Launch shapes and workspaces of paged attention with weights, with the launches recorded instead of made.  No GPU."""
+import pytest
+
+import test_launches_host
+
+RECORDER = test_launches_host.RECORDER.replace("if (block.x == 256)", "if (0)")
+
+ATTEND = """
+import ctypes as C, sys
+sys.modules["torch"] = None
+C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+import paper_2510_24606_amd as dhsa
+T, n_seq, dtype, pages, extra = map(int, sys.argv[2:])
+p = dhsa.dhsa_paged(T=T, n_seq=n_seq, H_q=32, H_kv=8, D=128, dtype=dtype, page_size=64, n_pages=pages, max_pages=512)
+at = 1 << 40                                          # an address that nothing reads
+code = dhsa.lib().dhsa_paged_attend(C.byref(p), at, at, at, at, at, at, at, None, at, 1.0, at, dhsa.dhsa_paged_workspace_bytes(p) + extra, None)
+assert code == 0, code
+"""
+
+
+@pytest.mark.parametrize("dtype,keys", [(0, 64), (1, 128)])
+@pytest.mark.parametrize("T,n_seq", [(2048, 1), (255 + 512, 256), (64, 64), (100, 10)])
+def test_weights_have_workgroups_for_scores_that_are_made_again(T, n_seq, dtype, keys, tmp_path, monkeypatch):
+    """Whether scores are kept is settled by the lengths, on the device: a launch has a workgroup for every share that may have to
+    be made again, or at least four for each of the 256 CUs."""
+    monkeypatch.setattr(test_launches_host, "RECORDER", RECORDER)
+    pages = 512
+    x, y, z, threads = test_launches_host.launches(ATTEND, tmp_path, T, n_seq, dtype, pages, 0)[-1]
+    assert (y, z, threads) == (1, 1, 256) and x >= min(1024, pages * 64 // keys * 8)
