@@ -1,6 +1,7 @@
 """Launch shapes and workspaces of paged attention with weights, with the launches recorded instead of made.  No GPU."""
 import pytest
 
+import paper_2510_24606_amd as dhsa
 import test_launches_host
 
 RECORDER = test_launches_host.RECORDER.replace("if (block.x == 256)", "if (0)")
@@ -27,3 +28,20 @@ def test_weights_have_workgroups_for_scores_that_are_made_again(T, n_seq, dtype,
     pages = 512
     x, y, z, threads = test_launches_host.launches(ATTEND, tmp_path, T, n_seq, dtype, pages, 0)[-1]
     assert (y, z, threads) == (1, 1, 256) and x >= min(1024, pages * 64 // keys * 8)
+
+
+def sizes(T, n_seq, dtype):
+    """Bytes with and without weights, and those of the references and sums that weights need in any case."""
+    p = dhsa.dhsa_paged(T=T, n_seq=n_seq, H_q=32, H_kv=8, D=128, dtype=dtype, page_size=64, n_pages=9100, max_pages=512)
+    return dhsa.dhsa_paged_workspace_bytes(p), dhsa.dhsa_paged_workspace_bytes(p, False), 8 * 32 * T + 255
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_no_room_for_scores_that_nobody_keeps(dtype):
+    """A single sequence of more than 32 rows a kv-head keeps none: neither type has room for them."""
+    for T in (9, 100, 2048):
+        full, bare, norm = sizes(T, 1, dtype)
+        assert full <= bare + norm, T
+    for T, n_seq in ((1, 1), (4, 1), (64, 64), (200, 64)):
+        full, bare, norm = sizes(T, n_seq, dtype)
+        assert full > bare + norm, (T, n_seq)
