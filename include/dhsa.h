@@ -424,7 +424,9 @@ dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, con
  * ws_dev: scratch of dhsa_paged_workspace_bytes(prob, weights) bytes (weights: 0 where weights_dev
  * is NULL), 16-byte aligned, nothing in which has to be set; calls that share it must be ordered.  The
  * size depends on T, n_seq, the head counts and D; with weights and few new tokens a sequence also on the
- * pool (4 bytes for each slot and query head and token of a sequence: scores that are not computed twice). */
+ * pool (4 bytes for each slot and query head and token of a sequence: scores that are not computed twice),
+ * so it may be smaller for more tokens.  A workspace that was sized for more tokens of as many sequences
+ * serves fewer all the same: scores that find no room are computed again. */
 dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev, const void *K_dev, const void *V_dev,
                               const int32_t *table_dev, const int32_t *q_start_dev, const int32_t *kv_len_dev,
                               void *O_dev, float *lse_dev, float *weights_dev, float decay, void *ws_dev,

@@ -46,6 +46,7 @@ __device__ __forceinline__ float2 norm_of(float m, float l) { return l > 0.f ? m
 
 constexpr int kIntMaxP = 0x7fffffff;
 constexpr int kFewRows = 32;
+constexpr int kFewMean = 16;                 // rows a kv-head and sequence in the mean up to which tiles are the smallest
 constexpr int kScoreUnitsMax = 1 << 24;      // 4 GiB; 64 times that fits 32 bits
 
 // One sequence as the kernels see it: whatever is in the arrays, rows stay below T and slots below slots_max.  What does not fit is

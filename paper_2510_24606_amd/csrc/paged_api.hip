@@ -94,8 +94,8 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
     return DHSA_OK;
 }
 
-// Workspace of dhsa_paged_attend in bytes.
-struct PagedWs { int64_t off_state, off_part, off_cut, off_norm, off_scores, bytes; };
+// Workspace of dhsa_paged_attend in bytes: what a call wants, and the least that it runs with.
+struct PagedWs { int64_t off_state, off_part, off_cut, off_norm, off_scores, bytes, least; };
 PagedWs paged_ws(SpanArgs *a, int D, int dtype, bool weights) {
     choose_tiles(a, dtype, true);
     const int64_t M = a->M;
@@ -118,6 +118,19 @@ PagedWs paged_ws(SpanArgs *a, int D, int dtype, bool weights) {
         a->score_units = (int)std::min<int64_t>(std::min(every, once) * a->H_kv, kScoreUnitsMax);
     }
     w.bytes = w.off_scores + (int64_t)a->score_units * 256;
+    // Room for scores makes the size fall where more tokens mean that fewer are kept.  A workspace of any larger T has to do: from T1
+    // on only what comes before the scores is needed, which never falls; below, that of T1 is enough.
+    w.least = w.bytes;
+    if (a->score_units > 0) {
+        const int64_t T1 = dtype == DHSA_BF16 ? ((int64_t)(kFewMean + 1) * a->n_seq + a->G - 1) / a->G : (int64_t)kFewRows * a->n_seq / a->G + 1;
+        if (a->T >= T1) {
+            w.least = w.off_scores;
+        } else {
+            SpanArgs b = *a;
+            b.T = T1;
+            w.least = std::min(w.bytes, paged_ws(&b, D, dtype, true).off_scores);
+        }
+    }
     return w;
 }
 
@@ -197,7 +210,8 @@ DHSA_API dhsa_status dhsa_paged_attend(const dhsa_paged *prob, const void *Q_dev
         odd_words({table_dev, q_start_dev, kv_len_dev, lse_dev, weights_dev}))
         return DHSA_ERR_ALIGN;
     const PagedWs w = paged_ws(&a, prob->D, prob->dtype, weights_dev != nullptr);
-    if (ws_bytes < (size_t)w.bytes) return DHSA_ERR_WORKSPACE;
+    if (ws_bytes < (size_t)w.least) return DHSA_ERR_WORKSPACE;
+    a.score_units = (int)std::min<uint64_t>(a.score_units, (ws_bytes - (size_t)w.off_scores) / 256);      // (least has what comes before)
     char *ws = static_cast<char *>(ws_dev);
     a.Q = Q_dev; a.K = K_dev; a.V = V_dev; a.O = O_dev; a.lse = lse_dev;
     a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev;

@@ -471,8 +471,8 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
 // 24.8 and 22.
 void choose_tiles(SpanArgs *a, int dtype, bool paged) {
     const int64_t rows = a->T * a->G, mean = rows / std::max(a->n_seq, 1);
-    a->M = mean > 16 && (paged || rows * a->H_kv >= 320 * 32) ? 32 : 16;
-    if (dtype == DHSA_BF16 && mean > 16 && (paged || rows * a->H_kv >= 144 * kTallRows)) a->M = kTallRows;
+    a->M = mean > kFewMean && (paged || rows * a->H_kv >= 320 * 32) ? 32 : 16;
+    if (dtype == DHSA_BF16 && mean > kFewMean && (paged || rows * a->H_kv >= 144 * kTallRows)) a->M = kTallRows;
     a->target = !paged ? 0 : a->M == kTallRows ? 512 : 1024;
     a->part_cap = paged ? 2 * a->target + a->H_kv : 0;
 }

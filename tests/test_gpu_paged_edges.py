@@ -110,3 +110,20 @@ def test_rows_behind_the_table_keep_their_places(n, over, window, sinks, dtype, 
             paged_plain.close(lse[2 * g:2 * g + 2, rows], z, t_z, "lse")
             page, slot = b.slots(1)
             paged_plain.close(W[page, g, slot], got, t_w, "weights")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_weights_in_a_workspace_of_more_tokens(dtype):
+    """Its room for scores is too small for those of all sequences; nothing behind it is written."""
+    b = Batch([(1, 16000)] * 20, 32, 2, 64, dtype, 16, window=9000, sinks=5)
+    more = dhsa.dhsa_paged.from_buffer_copy(b.prob)
+    more.T = 22 if dtype == BF16 else 41                # 17 (33) rows a kv-head and sequence in the mean
+    full, size = dhsa.dhsa_paged_workspace_bytes(b.prob), dhsa.dhsa_paged_workspace_bytes(more)
+    if dtype == F32:
+        size = min(size, dhsa.dhsa_paged_workspace_bytes(more, False) + 8 * 32 * more.T + 256)
+    assert size < full
+    whole = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+    W = b.new_weights()
+    before = W.clone()
+    b.check(*b.attend(W, 0.5, ws=whole[:size]), before, W, 0.5)
+    assert (whole[size:] == 77).all()

@@ -45,3 +45,27 @@ def test_no_room_for_scores_that_nobody_keeps(dtype):
     for T, n_seq in ((1, 1), (4, 1), (64, 64), (200, 64)):
         full, bare, norm = sizes(T, n_seq, dtype)
         assert full > bare + norm, (T, n_seq)
+
+
+ATTEND_IN_ANOTHER = """
+import ctypes as C, sys
+sys.modules["torch"] = None
+C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+import paper_2510_24606_amd as dhsa
+n_seq, dtype = map(int, sys.argv[2:])
+at = 1 << 40
+sizes = [1, 2, 7, 8, 9, 16, 17, 33, 64, 65, 100, 255, 256, 257, 300, 511, 512, 513, 528, 529, 600, 2048, 4096, 70000]
+probs = [dhsa.dhsa_paged(T=T, n_seq=n_seq, H_q=32, H_kv=8, D=128, dtype=dtype, page_size=64, n_pages=9100, max_pages=512) for T in sizes]
+attend = lambda p, n: dhsa.lib().dhsa_paged_attend(C.byref(p), at, at, at, at, at, at, at, None, at, 1.0, at, n, None)
+for i, p in enumerate(probs):
+    for q in probs[i:]:
+        assert attend(p, dhsa.dhsa_paged_workspace_bytes(q)) == 0, (p.T, q.T)
+    assert attend(p, dhsa.dhsa_paged_workspace_bytes(p, False)) == (6 if p.T else 0), p.T      # (weights need their own part in any case)
+"""
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("n_seq", [1, 3, 64, 1000])
+def test_a_workspace_of_more_tokens_serves_fewer(n_seq, dtype, tmp_path, monkeypatch):
+    monkeypatch.setattr(test_launches_host, "RECORDER", RECORDER)
+    assert test_launches_host.launches(ATTEND_IN_ANOTHER, tmp_path, n_seq, dtype)
