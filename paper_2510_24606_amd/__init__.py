@@ -447,6 +447,13 @@ def _same_cache(f, K, V, table, weights, dev: int):
         _same("weights", weights, torch.float32, pool[:3], dev, (H_kv * page, page, 1))
 
 
+def _scratch(ws, dev: int):
+    """Address and bytes of a workspace."""
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"workspace: strides {ws.stride()} on {ws.device}, where contiguous memory of the current device is wanted")
+    return ws.data_ptr(), ws.numel()
+
+
 def dhsa_paged_append(prob, K_new, V_new, K, V, table, q_start, kv_len, weights=None) -> None:
     """New rows K_new, V_new [H_kv, T, D] into the slots kv_len[s] - n_s .. kv_len[s] - 1 of their sequences; `weights` (float
     [n_pages, H_kv, page_size]) becomes 0 there."""
@@ -478,7 +485,7 @@ def dhsa_paged_attend(prob, Q, K, V, table, q_start, kv_len, O, ws, lse=None, we
     _check(lib().dhsa_paged_attend(_PAGED.pack(*f[:12], q[0], q[1], o[0], o[1], *f[16:]), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
                                    table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), O.data_ptr(),
                                    None if lse is None else lse.data_ptr(), None if weights is None else weights.data_ptr(), decay,
-                                   ws.data_ptr(), ws.numel(), _stream()))
+                                   *_scratch(ws, dev), _stream()))
 
 
 def dhsa_paged_evict(prob, K, V, weights, table, kv_len, keep: int, first: int, recent: int, ws, kv_len_out, table_out=None,
@@ -498,7 +505,7 @@ def dhsa_paged_evict(prob, K, V, weights, table, kv_len, keep: int, first: int, 
         _same("idx", idx, torch.int32, (n_seq, H_kv, keep), dev, (H_kv * keep, keep, 1))
     _check(lib().dhsa_paged_evict(_PAGED.pack(*f), K.data_ptr(), V.data_ptr(), weights.data_ptr(), table.data_ptr(), kv_len.data_ptr(),
                                   keep, first, recent, table_out.data_ptr(), kv_len_out.data_ptr(),
-                                  None if idx is None else idx.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+                                  None if idx is None else idx.data_ptr(), *_scratch(ws, dev), _stream()))
 
 
 def dhsa_version() -> int:
