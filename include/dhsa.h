@@ -364,7 +364,8 @@ dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t window, int64_
                                 const void *K_dev, const void *V_dev, void *O_dev, void *stream);
 
 /* K and V rows of several sequences in pages of one pool, and the new tokens of a call.
- *   K, V   [n_pages][H_kv][page_size][D], D contiguous, with the strides below
+ *   K, V   [n_pages][H_kv][page_size][D], D contiguous, with the strides below (where there is
+ *          but one page, head, slot or token its stride is not used, here and above)
  *   table  int32 [n_seq][max_pages], device: page of slots [p page_size, (p + 1) page_size)
  *          of a sequence.  A contiguous cache [H_kv][L][D] is one page of L slots.
  *   kv_len int32 [n_seq], device: tokens of each sequence, the new ones included; they are

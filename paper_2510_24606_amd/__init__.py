@@ -372,12 +372,15 @@ def dhsa_decode_step(prob, Q, K, V, B, ws, N_c_cap: int, L_cap: int, kc_valid: i
 
 def _same(what: str, t, dtype, shape, dev: int, strides=None):
     """The tensors of the calls below are described by one problem struct: what does not fit it is refused here.  strides: what
-    they have to be, None: any of contiguous rows (a stride of 0 would say packed).  Returns them."""
+    they have to be, None: any of contiguous rows (a stride of 0 would say packed); where there is but one of something its stride
+    is not looked at, here and in the library.  Returns them."""
     st = t.stride()
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, where {dtype} {tuple(shape)} on the current device is wanted")
     if st != strides if strides is not None else (st[-1] != 1 or 0 in st):
-        raise ValueError(f"{what}: strides {st}, where {strides or 'contiguous rows, none of them shared'} are wanted")
+        wrong = [x != y for x, y in zip(st, strides)] if strides is not None else [x == 0 for x in st[:-1]] + [st[-1] != 1]
+        if 0 not in shape and any(n > 1 and w for n, w in zip(shape, wrong)):
+            raise ValueError(f"{what}: strides {st}, where {strides or 'contiguous rows, none of them shared'} are wanted")
     return st
 
 

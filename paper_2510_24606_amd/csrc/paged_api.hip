@@ -45,9 +45,10 @@ dhsa_status heads(int64_t H_q, int64_t H_kv, int32_t D, int32_t dtype, float sca
     return DHSA_OK;
 }
 
-// A stride in elements: the default where it is 0, at least `least`, a multiple of 16 bytes.
-dhsa_status stride(int64_t in, int64_t packed, int64_t least, int esz, int64_t *out) {
-    *out = in ? in : packed;
+// A stride in elements between n of something: the default where it is 0 or nothing is that far apart, at least `least`, a
+// multiple of 16 bytes.
+dhsa_status stride(int64_t in, int64_t n, int64_t packed, int64_t least, int esz, int64_t *out) {
+    *out = in && n > 1 ? in : packed;
     if (*out < least || *out > INT64_MAX / 64) return DHSA_ERR_SHAPE;
     return (*out * esz) % 16 != 0 ? DHSA_ERR_ALIGN : DHSA_OK;
 }
@@ -69,15 +70,16 @@ dhsa_status resolve_paged(const dhsa_paged *in, SpanArgs *a, AppendArgs *ap) {
     const int esz = in->dtype == DHSA_F32 ? 4 : 2;
     const int64_t D = in->D, T = in->T, ps = in->page_size, H_kv = in->H_kv;
     int64_t ks_p, ks_h, ks_s, vs_p, vs_h, vs_s, kn_h, kn_t, vn_h, vn_t;
-    const struct { int64_t in, packed, least; int64_t *out; } all[] = {
-        {in->q_stride_h, std::max<int64_t>(T, 1) * D, 0, &a->qs_h}, {in->q_stride_t, D, D, &a->qs_t},
-        {in->o_stride_h, std::max<int64_t>(T, 1) * D, 0, &a->os_h}, {in->o_stride_t, D, D, &a->os_t},
-        {in->k_stride_p, H_kv * ps * D, D, &ks_p}, {in->k_stride_h, ps * D, 0, &ks_h}, {in->k_stride_s, D, D, &ks_s},
-        {in->v_stride_p, H_kv * ps * D, D, &vs_p}, {in->v_stride_h, ps * D, 0, &vs_h}, {in->v_stride_s, D, D, &vs_s},
-        {in->kn_stride_h, std::max<int64_t>(T, 1) * D, 0, &kn_h}, {in->kn_stride_t, D, D, &kn_t},
-        {in->vn_stride_h, std::max<int64_t>(T, 1) * D, 0, &vn_h}, {in->vn_stride_t, D, D, &vn_t}};
+    const int64_t H_q = in->H_q, np = in->n_pages;
+    const struct { int64_t in, n, packed, least; int64_t *out; } all[] = {
+        {in->q_stride_h, H_q, std::max<int64_t>(T, 1) * D, 0, &a->qs_h}, {in->q_stride_t, T, D, D, &a->qs_t},
+        {in->o_stride_h, H_q, std::max<int64_t>(T, 1) * D, 0, &a->os_h}, {in->o_stride_t, T, D, D, &a->os_t},
+        {in->k_stride_p, np, H_kv * ps * D, D, &ks_p}, {in->k_stride_h, H_kv, ps * D, 0, &ks_h}, {in->k_stride_s, ps, D, D, &ks_s},
+        {in->v_stride_p, np, H_kv * ps * D, D, &vs_p}, {in->v_stride_h, H_kv, ps * D, 0, &vs_h}, {in->v_stride_s, ps, D, D, &vs_s},
+        {in->kn_stride_h, H_kv, std::max<int64_t>(T, 1) * D, 0, &kn_h}, {in->kn_stride_t, T, D, D, &kn_t},
+        {in->vn_stride_h, H_kv, std::max<int64_t>(T, 1) * D, 0, &vn_h}, {in->vn_stride_t, T, D, D, &vn_t}};
     for (const auto &x : all)
-        if ((st = stride(x.in, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
+        if ((st = stride(x.in, x.n, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
     if (!fits(in->n_pages, ks_p, ps, ks_s, in->D, esz) || !fits(in->n_pages, vs_p, ps, vs_s, in->D, esz)) return DHSA_ERR_SHAPE;
     a->T = T;
     a->n_seq = in->n_seq;
@@ -150,12 +152,13 @@ DHSA_API dhsa_status dhsa_window_prefill(const dhsa_problem *prob, int64_t windo
     const int esz = prob->dtype == DHSA_F32 ? 4 : 2;
     const int64_t D = prob->D, L = prob->L;
     int64_t ks_h, ks_l, vs_h, vs_l;
-    const struct { int64_t in, packed, least; int64_t *out; } all[] = {
-        {prob->q_stride_h, L * D, 0, &a.qs_h}, {prob->q_stride_l, D, D, &a.qs_t}, {prob->k_stride_h, L * D, 0, &ks_h},
-        {prob->k_stride_l, D, D, &ks_l}, {prob->v_stride_h, L * D, 0, &vs_h}, {prob->v_stride_l, D, D, &vs_l},
-        {prob->o_stride_h, L * D, 0, &a.os_h}, {prob->o_stride_l, D, D, &a.os_t}};
+    const int64_t H_q = prob->H_q, H_kv = prob->H_kv;
+    const struct { int64_t in, n, packed, least; int64_t *out; } all[] = {
+        {prob->q_stride_h, H_q, L * D, 0, &a.qs_h}, {prob->q_stride_l, L, D, D, &a.qs_t}, {prob->k_stride_h, H_kv, L * D, 0, &ks_h},
+        {prob->k_stride_l, L, D, D, &ks_l}, {prob->v_stride_h, H_kv, L * D, 0, &vs_h}, {prob->v_stride_l, L, D, D, &vs_l},
+        {prob->o_stride_h, H_q, L * D, 0, &a.os_h}, {prob->o_stride_l, L, D, D, &a.os_t}};
     for (const auto &x : all)
-        if ((st = stride(x.in, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
+        if ((st = stride(x.in, x.n, x.packed, x.least, esz, x.out)) != DHSA_OK) return st;
     if (!fits(L, ks_l, 1, 0, prob->D, esz) || !fits(L, vs_l, 1, 0, prob->D, esz)) return DHSA_ERR_SHAPE;
     // (as dhsa_prefill: the bf16 rows of a head are addressed with 32-bit offsets)
     if (prob->dtype == DHSA_BF16 && (L * ks_l * 2 > (int64_t)1 << 32 || L * vs_l * 2 > (int64_t)1 << 32)) return DHSA_ERR_SHAPE;

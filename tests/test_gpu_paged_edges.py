@@ -127,3 +127,19 @@ def test_weights_in_a_workspace_of_more_tokens(dtype):
     before = W.clone()
     b.check(*b.attend(W, 0.5, ws=whole[:size]), before, W, 0.5)
     assert (whole[size:] == 77).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_strides_of_a_single_one(dtype):
+    """One sequence, token, head and page: their strides may say anything."""
+    from test_paged_edges_host import odd
+    b = Batch([(1, 37)], 1, 1, 64, dtype, 48, spare=0)
+    Kn, Vn = (odd(torch.randn((1, 1, 64), generator=b.g).to(dtype).cuda()) for _ in range(2))
+    b.K, b.V, b.Q, b.table = odd(b.K), odd(b.V), odd(b.Q), odd(b.table)
+    b.prob = dhsa.paged_problem(b.K, b.V, b.table, 1, 1)
+    W = odd(b.new_weights())
+    dhsa.dhsa_paged_append(b.prob, Kn, Vn, b.K, b.V, b.table, b.q_start, b.kv_len, W)
+    b.kc[0][:, 36], b.vc[0][:, 36] = Kn[:, 0].cpu(), Vn[:, 0].cpu()
+    before = W.clone()
+    assert (W[0, 0, 36] == 0).all()
+    b.check(*b.attend(W, 1.0), before, W, 1.0)

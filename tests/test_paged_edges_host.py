@@ -70,3 +70,49 @@ def test_a_workspace_of_another_device_or_with_gaps_is_refused(call, recorder):
         with pytest.raises(ValueError, match="workspace"):
             call(p, dict(t, ws=bad))
     assert len(recorder.calls) == 1
+
+
+def odd(t):
+    """The same tensor with a stride of 3 wherever there is but one of something."""
+    return t.as_strided(t.shape, [3 if n == 1 else x for n, x in zip(t.shape, t.stride())])
+
+
+@pytest.mark.parametrize("kw", [dict(n_seq=1), dict(T=1), dict(n_pages=1, width=1), dict(page=1), dict(H_q=1, H_kv=1),
+                                dict(n_seq=1, T=1, H_q=1, H_kv=1, page=1, n_pages=1, width=1)])
+def test_strides_of_a_single_one_do_not_matter(kw, recorder):
+    t, _ = tensors(**kw)
+    t = {n: odd(x) for n, x in t.items()}
+    p = dhsa.paged_problem(t["K"], t["V"], t["table"], t["Q"].shape[0], t["Q"].shape[1])
+    for call in (attend, append, evict):
+        call(p, t)
+    assert len(recorder.calls) == 3
+    L = t["K_new"].shape[1]
+    dhsa.dhsa_window_prefill(dhsa.problem(t["Q"], t["K_new"], [0, L], L, V=t["V_new"]), t["Q"], t["K_new"], t["V_new"], t["O"], 5)
+    for q in (t["Q"].expand(t["Q"].shape), t["Q"].transpose(0, 1).contiguous().transpose(0, 1)):
+        attend(p, dict(t, Q=q))
+
+
+def test_strides_that_matter_are_still_refused(recorder):
+    t, p = tensors()
+    for name, bad in (("table", torch.zeros((2, 9), dtype=torch.int32)[:, :3]), ("table", torch.zeros((3, 2), dtype=torch.int32).T),
+                      ("lse", torch.zeros((3, 4)).T), ("weights", torch.zeros((5, 16, 2)).transpose(1, 2)), ("Q", t["Q"][:, :1].expand(4, 3, 64)),
+                      ("K", t["K"][:, :1].expand(5, 2, 16, 64)), ("kv_len", torch.zeros(1, dtype=torch.int32).expand(2)),
+                      ("O", torch.zeros((4, 64, 3)).transpose(1, 2))):
+        with pytest.raises(ValueError, match=name):
+            attend(p, dict(t, **{name: bad}))
+    assert not recorder.calls
+
+
+def test_the_library_does_not_look_at_strides_of_a_single_one():
+    names = ["q_stride_t", "o_stride_t", "kn_stride_t", "vn_stride_t", "k_stride_p", "v_stride_p", "k_stride_s", "v_stride_s", "q_stride_h",
+             "o_stride_h", "k_stride_h", "v_stride_h", "kn_stride_h", "vn_stride_h"]
+    one = dict(T=1, n_seq=1, H_q=1, H_kv=1, D=64, dtype=dhsa.DHSA_BF16, page_size=1, n_pages=1, max_pages=1)
+    two = dict(one, T=2, H_q=2, H_kv=2, page_size=2, n_pages=2)
+    for name in names:
+        for x in (3, -8, 1 << 62):
+            assert dhsa.dhsa_paged_workspace_bytes(dhsa.dhsa_paged(**one, **{name: x})) > 0, name
+            assert dhsa.dhsa_paged_workspace_bytes(dhsa.dhsa_paged(**two, **{name: x})) == 0, name
+    for name in ("q_stride_h", "q_stride_l", "k_stride_h", "k_stride_l", "v_stride_h", "v_stride_l", "o_stride_h", "o_stride_l"):
+        codes = [dhsa.lib().dhsa_window_prefill(C.byref(dhsa.dhsa_problem(L=n, H_q=n, H_kv=n, D=64, dtype=dhsa.DHSA_BF16, **{name: 3})), 5, 0,
+                                                None, None, None, None, None) for n in (1, 2)]
+        assert codes[0] == 1 and codes[1] in (2, 9), name           # DHSA_ERR_NULL: all else is right
