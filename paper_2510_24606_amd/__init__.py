@@ -417,8 +417,13 @@ def dhsa_paged_workspace_bytes(prob: dhsa_paged, weights: bool = True) -> int:
     return int(lib().dhsa_paged_workspace_bytes(C.byref(prob), int(weights)))
 
 
+def _i32(n: int) -> int:
+    """A number of tokens as it goes to the library, which refuses both ends (ctypes would take the low 32 bits)."""
+    return max(-1, min(n, 0x7FFFFFFF))
+
+
 def dhsa_paged_evict_workspace_bytes(prob: dhsa_paged, keep: int) -> int:
-    return int(lib().dhsa_paged_evict_workspace_bytes(C.byref(prob), keep))
+    return int(lib().dhsa_paged_evict_workspace_bytes(C.byref(prob), _i32(keep)))
 
 
 def alloc_paged(prob: dhsa_paged, device="cuda", weights: bool = True):
@@ -507,7 +512,7 @@ def dhsa_paged_evict(prob, K, V, weights, table, kv_len, keep: int, first: int, 
     if idx is not None:
         _same("idx", idx, torch.int32, (n_seq, H_kv, keep), dev, (H_kv * keep, keep, 1))
     _check(lib().dhsa_paged_evict(_PAGED.pack(*f), K.data_ptr(), V.data_ptr(), weights.data_ptr(), table.data_ptr(), kv_len.data_ptr(),
-                                  keep, first, recent, table_out.data_ptr(), kv_len_out.data_ptr(),
+                                  _i32(keep), _i32(first), _i32(recent), table_out.data_ptr(), kv_len_out.data_ptr(),
                                   None if idx is None else idx.data_ptr(), *_scratch(ws, dev), _stream()))
 
 

@@ -116,3 +116,19 @@ def test_the_library_does_not_look_at_strides_of_a_single_one():
         codes = [dhsa.lib().dhsa_window_prefill(C.byref(dhsa.dhsa_problem(L=n, H_q=n, H_kv=n, D=64, dtype=dhsa.DHSA_BF16, **{name: 3})), 5, 0,
                                                 None, None, None, None, None) for n in (1, 2)]
         assert codes[0] == 1 and codes[1] in (2, 9), name           # DHSA_ERR_NULL: all else is right
+
+
+def test_numbers_of_tokens_do_not_lose_their_high_bits(recorder):
+    t, p = tensors()
+    for keep, first, recent in (((1 << 32) + 8, 0, 0), (8, (1 << 32) + 1, 0), (8, 0, -(1 << 32)), (-(1 << 32) + 8, 0, 0)):
+        dhsa.dhsa_paged_evict(p, t["K"], t["V"], t["weights"], t["table"], t["kv_len"], keep, first, recent, t["ws"], t["kv_out"])
+        got = [C.c_int32(x).value for x in recorder.calls[-1][1][6:9]]
+        code = C.CDLL(dhsa.LIB_PATH).dhsa_paged_evict(C.byref(p), None, None, None, None, None, *got, None, None, None, None, C.c_size_t(0), None)
+        assert code == 4, got                            # DHSA_ERR_BUDGET
+
+
+def test_a_budget_beyond_32_bits_has_no_workspace():
+    t, p = tensors()
+    assert dhsa.dhsa_paged_evict_workspace_bytes(p, 1 << 30) > 0
+    for keep in ((1 << 32) + 8, 1 << 31, -(1 << 32) + 8):
+        assert dhsa.dhsa_paged_evict_workspace_bytes(p, keep) == 0
