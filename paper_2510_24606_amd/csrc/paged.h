@@ -1,6 +1,7 @@
 // Shared by the translation units of attention without routing: windows and paged caches (see include/dhsa.h).
 #pragma once
 #include "dhsa_internal.h"
+#include "divide.h"
 
 namespace dhsa {
 
@@ -15,7 +16,7 @@ struct SpanArgs {
     int64_t T;
     int n_seq, H_kv, G;
     int n_pages, max_pages, page_size;
-    uint32_t div_mul;            // x / page_size = x div_mul >> div_shift for x < 2^31
+    uint32_t div_mul;            // of page_size (see divide.h)
     int div_shift;
     int window, sinks;           // window = INT_MAX: none
     int slots_max;               // max_pages page_size
@@ -30,7 +31,7 @@ struct SpanArgs {
     float *part;
     float2 *state;
     int2 *cut;
-    int g_shift;                 // R / G = R g_mul >> g_shift
+    int g_shift;                 // of G
     uint32_t g_mul;
     // scores of sequences of at most kFewRows rows a kv-head, for the weights (nullptr: none are kept): score_units times 64.  A
     // kv-head of a sequence has 64 ceil(kv / 64) for each row, its packed keys in blocks of 32, the rows of a block side by side
@@ -92,11 +93,11 @@ __device__ __forceinline__ int key_hi(const SpanArgs &a, int j) {
 }
 
 __device__ __forceinline__ int page_of(const SpanArgs &a, int slot) {
-    return (int)(((uint64_t)(uint32_t)slot * a.div_mul) >> a.div_shift);
+    return divided(slot, a.div_mul, a.div_shift);
 }
 
 __device__ __forceinline__ int token_of(const SpanArgs &a, int R) {
-    return (int)(((uint64_t)(uint32_t)R * a.g_mul) >> a.g_shift);
+    return divided(R, a.g_mul, a.g_shift);
 }
 
 // Blocks of kept scores that a sequence needs: 0 if none are kept of it.  Sequences get theirs one after another; one that

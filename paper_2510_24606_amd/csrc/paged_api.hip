@@ -22,15 +22,6 @@ bool odd_words(std::initializer_list<const void *> all) {
 }
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
-// x / d as a multiplication: with l = ceil(log2 d) and mul = floor(2^(31 + l) / d) + 1 < 2^32, mul d - 2^(31 + l) is
-// in 1 .. d <= 2^l, so x mul / 2^(31 + l) is above x / d by less than 1 / d for x < 2^31
-void set_divisor(uint32_t d, uint32_t *mul, int *shift) {
-    int l = 0;
-    while (((uint64_t)1 << l) < d) ++l;
-    *mul = (uint32_t)((((uint64_t)1 << (31 + l)) / d) + 1);
-    *shift = 31 + l;
-}
-
 // What the two problem structs have in common.
 dhsa_status heads(int64_t H_q, int64_t H_kv, int32_t D, int32_t dtype, float scale, SpanArgs *a) {
     if (dtype != DHSA_F32 && dtype != DHSA_BF16) return DHSA_ERR_DTYPE;
