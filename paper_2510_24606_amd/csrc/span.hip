@@ -394,11 +394,11 @@ __global__ __launch_bounds__(256, 2) void k_span(SpanArgs a, unsigned block0) {
 constexpr int kJoinRows = 4096;     // workgroups, as long as each has at most 64 rows
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per) {
+__global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per, int64_t row0) {
     constexpr int CPL = D / 16, U = 4;
     __shared__ float s_m[16], s_l[16], s_o[16][D];
     const int tid = threadIdx.x, lane = tid & 63, grp = tid >> 4, c0 = (tid & 15) * CPL;
-    const int64_t rows = a.T * a.H_kv * a.G, r0 = (int64_t)blockIdx.x * per;
+    const int64_t rows = a.T * a.H_kv * a.G, r0 = row0 + (int64_t)blockIdx.x * per;
     const int begin = a.q_start[0], end = a.q_start[a.n_seq];      // other rows are nobody's: what lies in `cut` means nothing
     int2 cut = make_int2(0, 0);
     const int t_me = (int)((r0 + lane) % a.T);
@@ -504,13 +504,17 @@ hipError_t launch_span(const SpanArgs &a, int D, int dtype, hipStream_t s) {
     if (a.target > 0) {
         const int64_t rows = a.T * a.H_kv * a.G;
         const int per = (int)std::min<int64_t>(64, (rows + kJoinRows - 1) / kJoinRows);
-        const dim3 grid((unsigned)((rows + per - 1) / per));
-#define DHSA_JOIN(T_, D_) hipLaunchKernelGGL((k_span_join<T_, D_>), grid, dim3(256), 0, s, a, per)
-        if (dtype == DHSA_F32) { if (D == 64) DHSA_JOIN(float, 64); else DHSA_JOIN(float, 128); }
-        else { if (D == 64) DHSA_JOIN(bf16_t, 64); else DHSA_JOIN(bf16_t, 128); }
+        for (int64_t r0 = 0; r0 < rows; r0 += (int64_t)kGridMax * per) {
+            const dim3 grid((unsigned)std::min<int64_t>((rows - r0 + per - 1) / per, kGridMax));
+#define DHSA_JOIN(T_, D_) hipLaunchKernelGGL((k_span_join<T_, D_>), grid, dim3(256), 0, s, a, per, r0)
+            if (dtype == DHSA_F32) { if (D == 64) DHSA_JOIN(float, 64); else DHSA_JOIN(float, 128); }
+            else { if (D == 64) DHSA_JOIN(bf16_t, 64); else DHSA_JOIN(bf16_t, 128); }
 #undef DHSA_JOIN
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace dhsa

@@ -69,3 +69,27 @@ for i, p in enumerate(probs):
 def test_a_workspace_of_more_tokens_serves_fewer(n_seq, dtype, tmp_path, monkeypatch):
     monkeypatch.setattr(test_launches_host, "RECORDER", RECORDER)
     assert test_launches_host.launches(ATTEND_IN_ANOTHER, tmp_path, n_seq, dtype)
+
+
+LARGE = """
+import ctypes as C, sys
+sys.modules["torch"] = None
+C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+import paper_2510_24606_amd as dhsa
+T, heads = map(int, sys.argv[2:])
+p = dhsa.dhsa_paged(T=T, n_seq=1, H_q=heads, H_kv=heads, D=64, dtype=1, page_size=64, n_pages=64, max_pages=64)
+at = 1 << 40
+assert dhsa.lib().dhsa_paged_attend(C.byref(p), at, at, at, at, at, at, at, None, None, 1.0, at, dhsa.dhsa_paged_workspace_bytes(p, False), None) == 0
+"""
+
+
+@pytest.mark.parametrize("T,heads", [(1 << 23, 64), (1 << 24, 64), ((1 << 24) + 77, 64), (1 << 25, 32)])
+def test_grids_of_very_many_rows(T, heads, tmp_path, monkeypatch):
+    """Rows beyond what 2^32 threads join (64 a workgroup of 256), tiles beyond what they attend."""
+    recorder = test_launches_host.RECORDER.replace("if (block.x == 256)", "if (0)")
+    recorder = recorder.replace('printf("\\n");', 'printf(" %d\\n", *(int *)args[1]);')          # 64 rows a workgroup marks a join
+    monkeypatch.setattr(test_launches_host, "RECORDER", recorder)
+    made = test_launches_host.launches(LARGE, tmp_path, T, heads)
+    assert all(x * threads < 1 << 32 and (y, z) == (1, 1) for x, y, z, threads, _ in made)
+    joined = sum(x for x, *_, per in made if per == 64)
+    assert joined * 64 >= T * heads > joined * 64 - 64
