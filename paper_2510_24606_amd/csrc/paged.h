@@ -63,11 +63,11 @@ __device__ __forceinline__ Seq read_seq(const SpanArgs &a, int s) {
     int b = a.q_start[s], e = a.q_start[s + 1], kv = a.kv_len[s];
     const int T = (int)a.T;
     b = b < 0 ? 0 : b > T ? T : b;
-    const int64_t base = (int64_t)kv - e + b;            // the row before e has slot kv - 1
+    kv = kv < 0 ? 0 : kv;
+    q.base = e > b ? kv - (e - b) : 0;                   // the row before e has slot kv - 1
     e = e < b ? b : e > T ? T : e;
-    kv = kv < 0 ? 0 : kv > a.slots_max ? a.slots_max : kv;
+    kv = kv > a.slots_max ? a.slots_max : kv;
     q.q0 = b; q.n = e - b; q.kv = kv;
-    q.base = base < -q.n ? -q.n : q.n == 0 ? 0 : (int)base;     // (below -n: all rows see nothing, however far below)
     return q;
 }
 
@@ -134,13 +134,13 @@ __device__ __forceinline__ bool find_item(const SpanArgs &a, unsigned b, int M, 
     const int lane = threadIdx.x & 63;
     const int g = (int)(b % (unsigned)a.H_kv), want = (int)(b / (unsigned)a.H_kv);
     int P = kIntMaxP;
+    const int t_in = (M + a.G - 1) / a.G + 1;                           // most tokens a tile touches
     const auto measure = [&](int s, Seq *q, int *tiles, int *units) {
         *tiles = *units = 0;
         q->n = 0;
         if (s >= a.n_seq) return;
         *q = read_seq(a, s);
-        *tiles = (int)(((int64_t)q->n * a.G + M - 1) / M);
-        const int t_in = (M + a.G - 1) / a.G + 1;                       // most tokens a tile touches
+        *tiles = (int)(((unsigned)(q->n * a.G) + (M - 1)) / M);         // (n G < 2^31)
         const int p1 = q->base + q->n - 1, p0 = p1 - t_in + 1 > 0 ? p1 - t_in + 1 : 0;
         *units = (make_span(a, p0, p1, q->kv).total + U - 1) / U;
     };
