@@ -8,7 +8,7 @@ namespace dhsa {
 // ---------------------------------------------------------------------------
 // Append: a workgroup per new token moves its rows of all kv-heads, 16 bytes a thread.  Bound by a chain of three loads (the
 // sequence of the token, its length, the page) where tokens are few (64 tokens of 8 kv-heads of 128, bf16: 3.0 us of kernel), by the
-// copy where they are many (24K tokens, 195 MB: 38.6 us, 5.1 TB/s).
+// copy where they are many (24K tokens, 195 MB: 38.2 us, 5.1 TB/s).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_append(SpanArgs a, AppendArgs ap, int row16, int t0) {
     const int t = t0 + blockIdx.x, lane = threadIdx.x & 63;
@@ -57,7 +57,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
 
-// A wave has consecutive slots, 64 at a time; IT times 1024 slots keep their keys in registers (what is longer reads them again).
+// A wave has consecutive slots, 64 at a time; IT times 1024 slots keep their keys in registers (of IT = 32 the rounds' conditions spill
+// 226 scalar registers into lanes of vector registers).  What is longer reads them again in each of five passes, page and weight one
+// after the other: a list of 131072 takes 300 us.
 // 8 x 8 lists of up to 32768 slots: 83 us with the keys read five times, by page and slot each time.
 template <int IT>
 __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, EvictArgs e) {
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(SpanArgs a, Evic
 // Eviction, second launch: the rows move.  In place one workgroup does its columns of a head: kept slots ascend, so row t moves
 // from a slot >= t; batches are read whole before they are written, and a batch is written below everything that a later one
 // reads.  Into other pages every batch has a workgroup of its own: 8 x 8 heads, 4096 rows each of K and V, 268 MB read and written,
-// 50 us (5.3 TB/s); in place 55 us.
+// 50 us (5.3 TB/s); in place, where a head's columns are one workgroup's, 67 us.
 // blockIdx.x: part (K columns, V columns, weights) and batch, y: kv-head, z: sequence.
 // ---------------------------------------------------------------------------
 constexpr int kMoveU = 4;

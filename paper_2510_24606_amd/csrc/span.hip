@@ -14,8 +14,8 @@
 //   fp32, BK = 16 (v_mfma_f32_16x16x4_f32): K as 16 bytes at 16 s + 4 q, V as 16 bytes at 64 t + 4 n of key 4 q + i.  Row m
 //   of output block (t, j) is column 64 t + 4 m + j.
 //
-// Tiles of 16 rows over a long cache are bound by the memory: 64 conversations of 578K tokens, 2.37 GB of K and V, 389 us (6.1 TB/s);
-// one of 128K tokens 90 us (6.0 TB/s).  Tiles of a short prompt by chains of loads and, in fp32, by the matrix unit: 1021 tokens of 4 heads
+// Tiles of 16 rows over a long cache are bound by the memory: 64 conversations of 578K tokens, 2.37 GB of K and V, 375 us (6.3 TB/s);
+// one of 128K tokens 89 us (6.0 TB/s).  Tiles of a short prompt by chains of loads and, in fp32, by the matrix unit: 1021 tokens of 4 heads
 // of 64, a window of 256 8.8 us a call.
 #include <algorithm>
 
@@ -32,7 +32,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
 __device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
 
-// What the two types differ in.  NC: columns of an output row that a lane has per output row m, all adjacent.
+// What the two types differ in.
 template <typename T, int D, int RB> struct Tile;
 
 template <int D, int RB> struct Tile<bf16_t, D, RB> {
@@ -48,8 +48,9 @@ template <int D, int RB> struct Tile<bf16_t, D, RB> {
 #pragma unroll
         for (int t = 0; t < NT; ++t) qf[r][t] = *reinterpret_cast<const bf16x8_t *>(row + 64 * t + 16 * q);
     }
-    // Offsets (16 bytes) of the block's rows are in LDS.  ONCE: nobody else reads these rows soon, so they go past the caches (64
-    // conversations of 578K tokens, K and V 2.4 GB: 427 -> 389 us).
+    // Offsets (16 bytes) of the block's rows are in LDS.  ONCE: a sequence of one tile has these rows for itself, so they go past the
+    // caches (64 conversations of 578K tokens, K and V 2.4 GB: 427 -> 389 us).  A longer chunk among single tokens, whose many tiles
+    // all read the same rows, pays for it: 512 tokens behind 30K of them 279 us alone, 1810 more among 255 single tokens.
     template <typename V_, bool ONCE> __device__ static V_ get(const char *p) {
         if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V_ *>(p));
         else return *reinterpret_cast<const V_ *>(p);
@@ -464,11 +465,15 @@ __global__ __launch_bounds__(256) void k_span_join(SpanArgs a, int per, int64_t 
 // Rows of a tile, us of the two sides.
 // bf16, paged (K and V pass once a tile): 128 rows from 17 rows a kv-head and sequence on; of 32 rows, 16 sequences of 4096 tokens,
 // 32-row tiles 64 and 128-row tiles 44; one of 32768 37 and 24; of 36 rows 88 and 45.  Up to 16 rows the few wide loads of 16-row
-// tiles keep the memory busy.
+// tiles keep the memory busy.  The mean decides for the whole call, so a batch of single tokens and a chunk has one side's tiles for
+// both: 255 tokens (2.19M cached) and a chunk of 512 behind 30K 3347, alone 1535 and 279; 63 tokens (445K) and one of 2048 behind 6144
+// 670, alone 304 and 252.
 // bf16, one prompt: 128 rows from 144 tiles on: 2000 tokens, 8 heads of 2 kv-heads (125 tiles), a window of 2000 36 with smaller
 // tiles, 44 with 128 rows; 3500 tokens, a window of 300 26 and 17.
-// Else 32 rows, if they make 320 tiles: fp32, 4 heads of 64, a window of 256, 1021 tokens 16 rows 9.9 and 32 rows 13.6; 4000 tokens
-// 24.8 and 22.
+// Else 32 rows from 17 rows a kv-head and sequence on; one prompt, if they make 320 tiles: fp32, 4 heads of 64, a window of 256, 1021
+// tokens 16 rows 9.9 and 32 rows 13.6; 4000 tokens 24.8 and 22.  fp32, paged, without that limit, groups of four: 16 sequences of 4096
+// tokens, 8 kv-heads of 128, 5 new tokens 16 rows 135 and 32 rows 116, 64 tokens 812 and 622; 2 kv-heads of 64, 5 tokens 32 and 30, 16
+// tokens 41 and 47 (the one of 24 such pairs that is worse than 3 %); one sequence of 32768, 5 tokens 89 and 71, 512 tokens 3129 and 2379.
 void choose_tiles(SpanArgs *a, int dtype, bool paged) {
     const int64_t rows = a->T * a->G, mean = rows / std::max(a->n_seq, 1);
     a->M = mean > kFewMean && (paged || rows * a->H_kv >= 320 * 32) ? 32 : 16;

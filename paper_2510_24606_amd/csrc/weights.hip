@@ -9,8 +9,9 @@
 //     has 16 keys of one row: it adds up its own keys over its rows, and the 32 rows of a block follow once at the end.  Bound
 //     by the vector unit: an exponential, a product and two sums a pair beside 16 cycles of matrix unit for 64 pairs.
 //     fp32: 64 keys in the registers of every wave, each of which takes every fourth block of 16 rows.
-// Kept scores of 64 conversations (74 MB, 578K tokens of 8 kv-heads) 32 us; computing them again from K would read 1.2 GB, 215 us.
-// 5718 new tokens of 12 sequences, groups of seven heads, a window of 4096: 215-270 us (vector unit busy 63 % of the cycles).
+// Kept scores of 64 conversations (74 MB, 578K tokens of 8 kv-heads) 31 us; computing them again from K would read 1.2 GB, 215 us.
+// 5718 new tokens of 12 sequences, groups of seven heads, a window of 4096: 249 us (vector unit busy 63 % of the cycles).  fp32, 1024
+// tokens behind 7168, 32 heads of 8 kv-heads of 128: 567 us (114 TFLOP/s).
 #include <algorithm>
 
 #include "attn_mfma.h"
@@ -26,8 +27,8 @@ constexpr int kKeptKeys = 4096;
 constexpr int kStages = 3;       // of 64 rows in LDS: two are on their way while one is worked on
 
 template <typename T> struct Heavy;
-template <> struct Heavy<bf16_t> { static constexpr int kKeys = 128, kRows = 64; };
-template <> struct Heavy<float> { static constexpr int kKeys = 64, kRows = 16; };
+template <> struct Heavy<bf16_t> { static constexpr int kKeys = 128; };
+template <> struct Heavy<float> { static constexpr int kKeys = 64; };
 
 template <typename T, int D> struct WeightsSmem;
 template <int D> struct WeightsSmem<bf16_t, D> {
