@@ -416,7 +416,8 @@ dhsa_status dhsa_paged_append(const dhsa_paged *prob, const void *K_new_dev, con
 /* Attention of the new tokens over the cache, their own rows included (append them first).
  * lse_dev (may be NULL): float [H_q][T], log of the sum of exp(q . k scale) over the row's
  * keys.  A row without keys gets O = 0 and lse = -infinity; a row of Q with a NaN in it NaN in
- * both and in the weights of the keys that it sees, and in nothing else.
+ * both and in the weights of the keys that it sees, and in nothing else.  O must not overlap Q:
+ * weights may be made from Q after O is there.
  * weights_dev (may be NULL): float [n_pages][H_kv][page_size], what each cached key has got of
  * attention: for every slot of the call's sequences
  *   weights = decay weights + sum over the call's rows and the query heads of the kv-head of

@@ -101,7 +101,7 @@ PagedWs paged_ws(SpanArgs *a, int D, int dtype, bool weights) {
     w.off_scores = w.off_norm + (weights ? up256(rows * 8) : 0);
     // Scores that are kept for the weights: every slot of the pool once, for as many rows as a sequence has in the mean (a
     // step of a batch has the same number of each).  What does not fit is computed again.  Where the mean is no longer few
-    // rows one sequence has more and keeps none (63 single tokens and a chunk of 2048 in fp32: 4.9 ms, 6.0 with none kept).
+    // rows one sequence has more and keeps none (63 single tokens of 1000..32000 and a chunk of 2048 in fp32: 4.9 ms, 6.0 with none kept).
     a->score_units = 0;
     if (weights && a->M <= kFewRows && a->T > 0 && a->n_seq > 0) {
         const int64_t mean = (a->T * a->G + a->n_seq - 1) / a->n_seq, pool = (int64_t)a->n_pages * a->page_size;
